@@ -155,6 +155,106 @@ int ts_densify_range(const int32_t* const* ids_k, const void* const* rows_k, con
                      const float* dense_in, float* dense_out, void* stream);
 
 /*
+ * Dropout.  A transformer drops elements of its embedded tokens (Section 5 trains that model); the gradient that
+ * reaches ts_densify as value rows is then zero in the same places.  Which elements those are is never stored: element
+ * e = t * d + j of row t, column j of a call's [n, d] array has a 32-bit word of its own, word e % 4 of Philox4x32 with
+ * seven rounds (Salmon et al., SC 2011) under the counter (e / 4 in its low and high 32 bits, o low, o high) and the key
+ * (seed low, seed high), and is kept if that word is at least floor(p * 2^32).  Kept elements are multiplied by
+ * 1 / (1 - p), dropped ones are +0.0 whatever they were (NaN and infinities included).  o = offset + *step: step is a
+ * device pointer to one 8-byte aligned number that the kernels read when they run (a captured graph whose program adds
+ * to it between replays gets a new mask each time), or NULL.  The same mask again -- the backward pass, or activations
+ * computed twice -- is the same call with the same seed and o.  0 <= p < 1, else TS_ERR_SHAPE; with p = 0 no word is
+ * made.  The struct is read before the call returns.
+ */
+typedef struct {
+    uint64_t seed;
+    uint64_t offset;
+    const uint64_t* step;
+    float p;
+    int32_t reserved;
+} ts_dropout_mask;
+
+/*
+ * out = add + dropout(x) over [n, d], fp32 (TS_ROW_FP32) or bf16 (TS_ROW_BF16) alike; add (the residual) may be NULL.
+ * Computed in fp32 and rounded once.  Its backward pass is the same call on the gradient of out, without add (the
+ * gradient of add is that of out).  out may be x or add; other overlaps are undefined.  d % 4 == 0; x, add and out are
+ * 16-byte aligned; n may be 0.
+ */
+int ts_dropout(const void* x, const void* add, int64_t n, int32_t d, int32_t dtype, const ts_dropout_mask* mask,
+               void* out, void* stream);
+
+/*
+ * The embedding lookup in front of the network, with the positions and the dropout that follow it:
+ *
+ *     out[t, :] = dropout(scale * weight[ids[t], :] + pos[pos_ids[t], :]),   t < n
+ *
+ * weight [V, d] and pos [n_pos, d] have one type (weight_dtype: TS_ROW_FP32 or TS_ROW_BF16), out [n, d] has its own
+ * (TS_OUT_FP32 or TS_OUT_BF16); fp32 in between, rounded once.  pos and pos_ids may both be NULL, with n_pos = 0.  An id
+ * outside [0, V) (padding: -1, say) or a position outside [0, n_pos) is not dereferenced and adds nothing.  Gradient of
+ * the weight: ts_densify_dropout on the gradient of out, with the same ids, scale and mask; of pos: the same with
+ * pos_ids, n_pos for V and a scale of 1.  out must not overlap the inputs.  d % 4 == 0; weight, pos and out are 16-byte
+ * aligned; n may be 0; scale is finite.
+ */
+int ts_lookup_dropout(const int32_t* ids, int64_t n, const void* weight, int32_t weight_dtype, int32_t d, int32_t V,
+                      float scale, const void* pos, const int32_t* pos_ids, int32_t n_pos, const ts_dropout_mask* mask,
+                      void* out, int32_t out_dtype, void* stream);
+
+/*
+ * ts_densify (row_dtype TS_ROW_FP32 or TS_ROW_BF16) with value rows that are the gradient of ts_lookup_dropout's out:
+ *
+ *     dense_out[v, :] = dense_in[v, :] + sum over pairs t with ids[t] == v of mask(t, :) * scale / (1 - p) * rows[t, :]
+ *
+ * The mask is made as the value rows are read.  Each kept element is multiplied once in fp32 by scale / (1 - p), rounded
+ * to fp32; the products are added in ts_densify's order.  scale finite, and so is scale / (1 - p), else TS_ERR_SHAPE.
+ * Everything else as for ts_densify, which is the case p = 0, scale = 1.
+ */
+int ts_densify_dropout(const int32_t* ids, const void* rows, int64_t n, int32_t row_dtype, int32_t d, int32_t V,
+                       float scale, const ts_dropout_mask* mask, const float* dense_in, float* dense_out, void* stream);
+
+/*
+ * Products in 8-bit floating point, for the pre-softmax projection: its logits H W^T and, in the backward pass, dL W and
+ * dL^T H -- the last is the dense gradient that the densify calls take as dense_in.  All three are A B^T of operands
+ * whose rows lie along the contracted axis.
+ *
+ * An operand [rows, K] is held as codes [rows, K rounded up to 128], one byte each (OCP e4m3 without infinities, or
+ * e5m2), what is beyond K zero, and as scales, one byte s for each block of 128 codes of a row, whose values are then
+ * code * 2^(s - 127): [rows, number of blocks rounded up to 4], bytes beyond the last block zero.  Both are row-major
+ * and contiguous; ts_fp8_layout returns the two row lengths.
+ */
+enum { TS_FP8_E4M3 = 0, TS_FP8_E5M2 = 1 };
+#define TS_FP8_BLOCK 128
+int ts_fp8_layout(int64_t K, int64_t* code_bytes, int64_t* scale_bytes);
+
+/*
+ * Codes and scales of x [rows, cols] (TS_ROW_FP32 or TS_ROW_BF16, contiguous), in one reading of x: q, q_scales hold x
+ * with blocks along its columns; qt, qt_scales hold its transpose [cols, rows] with blocks along the rows of x.  Either
+ * pair may be NULL, not both.  The scale of a block is the smallest power of two, 2^-127 at least, that brings its
+ * largest finite magnitude to at most 448 (e4m3) or 57344 (e5m2); codes are rounded to nearest, ties to even, so no
+ * finite value becomes infinite.  NaN stays NaN; an infinity becomes NaN in e4m3 and stays one in e5m2.  q, qt: 16-byte
+ * aligned, scales: 4-byte aligned, x: 16-byte aligned; rows or cols may be 0 (then nothing is written).
+ */
+int ts_quantize_fp8(const void* x, int32_t x_dtype, int64_t rows, int64_t cols, int32_t format,
+                    uint8_t* q, uint8_t* q_scales, uint8_t* qt, uint8_t* qt_scales, void* stream);
+
+/*
+ * out[m, n] = c_in[m, n] + sum over k of A[m, k] B[n, k],  m < M, n < N, k < K
+ *
+ * a, a_scales: A [M, K]; b, b_scales: B [N, K]; formats TS_FP8_*, one for each; a scale byte of 255 stands for NaN.
+ * Sums are fp32, in an order that follows from M, N and K alone: the same inputs give the same bits on every run.  out
+ * [M, N] is TS_OUT_FP32, made from exact products, or TS_OUT_BF16, made by the 8-bit matrix instructions, which cut what a
+ * product has more than 13 bits below the largest of its group of eight along K (1.5e-5 of the result's norm on normal
+ * data), and rounded once; c_in must be NULL with TS_OUT_BF16, else TS_ERR_SHAPE.  c_in fp32 [M, N] or NULL; it may be
+ * out.  M, N or K may be 0 (K = 0: out = c_in or zeros).  a, b: 16-byte aligned, scales: 4-byte, out and c_in: 16-byte.  M, N
+ * below 2^31, K at most 2^24.
+ * A product of few rows and columns is split along K and uses the bound workspace, ts_matmul_workspace_bytes(M, N, K)
+ * bytes of it (0 where it is not split); what ts_last_views described in that workspace is then gone.
+ */
+int ts_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t* bytes);
+int ts_matmul_fp8(const uint8_t* a, const uint8_t* a_scales, int32_t a_format,
+                  const uint8_t* b, const uint8_t* b_scales, int32_t b_format,
+                  int64_t M, int64_t N, int64_t K, const float* c_in, void* out, int32_t out_dtype, void* stream);
+
+/*
  * Host arithmetic, no GPU: where a [V, d] result of out_dtype goes in a fusion buffer of
  * capacity_bytes of which used_bytes are taken.  *offset_bytes = used_bytes rounded up to
  * 256; *used_after_bytes = offset + 4*V*d (2*V*d for bf16).  TS_ERR_CAPACITY if that

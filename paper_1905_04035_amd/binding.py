@@ -24,6 +24,7 @@ TS_RULE_TF, TS_RULE_PROPOSED = 1, 2
 TS_ACC_PASS_THROUGH, TS_ACC_REDUCE, TS_ACC_DENSIFY_REDUCE, TS_ACC_GATHER = 0, 1, 2, 3
 TS_ROW_FP32, TS_ROW_BF16 = 0, 1
 TS_OUT_FP32, TS_OUT_BF16 = 0, 1
+TS_FP8_E4M3, TS_FP8_E5M2, TS_FP8_BLOCK = 0, 1, 128
 TS_MAX_SHARDS = 64
 
 # TS_SANITIZE=1 selects the builds whose host code runs under ASan + UBSan (build.py, sanitize=True)
@@ -39,6 +40,20 @@ class TsGrad(C.Structure):
     """ts_grad of include/ts_densify.h."""
     _fields_ = [("kind", C.c_int32), ("reserved", C.c_int32), ("ids", C.c_void_p), ("values", C.c_void_p),
                 ("n", C.c_int64)]
+
+
+class TsDropoutMask(C.Structure):
+    """ts_dropout_mask of include/ts_densify.h."""
+    _fields_ = [("seed", C.c_uint64), ("offset", C.c_uint64), ("step", C.c_void_p), ("p", C.c_float), ("reserved", C.c_int32)]
+
+
+class DropoutMask:
+    """Which elements a call drops (ts_dropout_mask): the probability p, the key `seed` and, among the masks of one key, the
+    number offset + step[0].  step: None, or an int64 tensor of one element on the GPU, read when the kernels run."""
+    __slots__ = ("p", "seed", "offset", "step")
+
+    def __init__(self, p: float, seed: int, offset: int = 0, step: Optional[torch.Tensor] = None):
+        self.p, self.seed, self.offset, self.step = p, seed, offset, step
 
 
 class TsError(RuntimeError):
@@ -63,6 +78,13 @@ def lib():
         l.ts_densify_scaled.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp, vp, i32, C.c_float, vp]
         l.ts_fusion_place.argtypes = [i64, i64, i32, i32, i32, vp, vp]
         l.ts_densify_range.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp]
+        l.ts_dropout.argtypes = [vp, vp, i64, i32, i32, vp, vp, vp]
+        l.ts_lookup_dropout.argtypes = [vp, i64, vp, i32, i32, i32, C.c_float, vp, vp, i32, vp, vp, i32, vp]
+        l.ts_densify_dropout.argtypes = [vp, vp, i64, i32, i32, i32, C.c_float, vp, vp, vp, vp]
+        l.ts_fp8_layout.argtypes = [i64, vp, vp]
+        l.ts_quantize_fp8.argtypes = [vp, i32, i64, i64, i32, vp, vp, vp, vp, vp]
+        l.ts_matmul_workspace_bytes.argtypes = [i64, i64, i64, vp]
+        l.ts_matmul_fp8.argtypes = [vp, vp, i32, vp, vp, i32, i64, i64, i64, vp, vp, i32, vp]
         l.ts_buffer_bytes.argtypes = [i64, i64, i32, i32, i32, vp, vp]
         l.ts_accumulate_strategy.argtypes = [vp, i32, i32, vp]
         l.ts_accumulate.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, i64, vp, vp, vp]
@@ -83,14 +105,16 @@ def lib():
         l.ts_status_string.restype = C.c_char_p
         for name in ("ts_densify", "ts_densify_static", "ts_densify_bf16", "ts_densify_multi", "ts_buffer_bytes",
                      "ts_densify_scaled", "ts_fusion_place", "ts_densify_range",
-                     "ts_accumulate_strategy", "ts_accumulate",
+                     "ts_accumulate_strategy", "ts_accumulate", "ts_dropout", "ts_lookup_dropout", "ts_densify_dropout",
+                     "ts_fp8_layout", "ts_quantize_fp8", "ts_matmul_workspace_bytes", "ts_matmul_fp8",
                      "ts_workspace_bytes", "ts_call_workspace_bytes", "ts_bind_workspace", "ts_last_views", "ts_read_views", "ts_unique_ids",
                      "ts_last_launch_info",
                      "ts_profile_begin", "ts_profile_end", "ts_set_piece_tokens", "ts_set_overlap_bytes", "ts_set_sort_part", "ts_set_short_rows"):
             getattr(l, name).restype = C.c_int
         # what the extension module calls: addresses of the entry points
         for name in ("ts_densify", "ts_densify_static", "ts_densify_bf16", "ts_densify_multi", "ts_densify_scaled",
-                     "ts_densify_range", "ts_accumulate", "ts_accumulate_strategy"):
+                     "ts_densify_range", "ts_accumulate", "ts_accumulate_strategy", "ts_dropout", "ts_lookup_dropout",
+                     "ts_densify_dropout", "ts_quantize_fp8", "ts_matmul_fp8"):
             setattr(l, "at_" + name, C.cast(getattr(l, name), C.c_void_p).value)
         _lib = l
     return _lib
@@ -186,6 +210,61 @@ def ts_densify_range(ids_k: Sequence[torch.Tensor], rows_k: Sequence[torch.Tenso
     l, m = lib(), _marshal or marshal()
     _check(m.range(l.at_ts_densify_range, ids_k, rows_k, row_dtype, d, V, v_begin, v_end, dense_in, dense_out, stream),
            "ts_densify_range")
+
+
+def ts_dropout(x: torch.Tensor, mask: DropoutMask, out: torch.Tensor, add: Optional[torch.Tensor] = None, stream=None) -> None:
+    """out = add + dropout(x); x, add, out: [n, d], all float32 or all bfloat16 (or 16-bit integers that hold its bits)."""
+    l, m = lib(), _marshal or marshal()
+    _check(m.dropout(l.at_ts_dropout, x, mask, out, add, stream), "ts_dropout")
+
+
+def ts_lookup_dropout(ids: torch.Tensor, weight: torch.Tensor, scale: float, mask: DropoutMask, out: torch.Tensor,
+                      pos: Optional[torch.Tensor] = None, pos_ids: Optional[torch.Tensor] = None, stream=None) -> None:
+    """out[t] = dropout(scale * weight[ids[t]] + pos[pos_ids[t]])."""
+    l, m = lib(), _marshal or marshal()
+    _check(m.lookup(l.at_ts_lookup_dropout, ids, weight, scale, mask, out, pos, pos_ids, stream), "ts_lookup_dropout")
+
+
+def ts_densify_dropout(ids: torch.Tensor, rows: torch.Tensor, d: int, V: int, scale: float, mask: DropoutMask,
+                       dense_in: Optional[torch.Tensor], dense_out: torch.Tensor, stream=None) -> None:
+    """The gradient of ts_lookup_dropout's weight, added to dense_in; rows [n, d]: the gradient of its out."""
+    l, m = lib(), _marshal or marshal()
+    _check(m.densify_dropout(l.at_ts_densify_dropout, ids, rows, d, V, scale, mask, dense_in, dense_out, stream),
+           "ts_densify_dropout")
+
+
+def ts_fp8_layout(K: int):
+    """(bytes of a row of codes, bytes of a row of scales) of an operand [rows, K]."""
+    codes, scales = C.c_int64(0), C.c_int64(0)
+    _check(lib().ts_fp8_layout(K, C.byref(codes), C.byref(scales)), "ts_fp8_layout")
+    return codes.value, scales.value
+
+
+def fp8_empty(rows: int, K: int, fmt: int = TS_FP8_E4M3, device="cuda:0"):
+    """Uninitialised (codes, scales) of an operand [rows, K] for ts_quantize_fp8 to fill."""
+    codes, scales = ts_fp8_layout(K)
+    return (torch.empty(rows, codes, dtype=torch.float8_e5m2 if fmt == TS_FP8_E5M2 else torch.float8_e4m3fn, device=device),
+            torch.empty(rows, scales, dtype=torch.uint8, device=device))
+
+
+def ts_quantize_fp8(x: torch.Tensor, fmt: int, q: Optional[torch.Tensor] = None, q_scales: Optional[torch.Tensor] = None,
+                    qt: Optional[torch.Tensor] = None, qt_scales: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Codes and scales of x [rows, cols] (q) and of its transpose (qt); fp8_empty makes either pair."""
+    l, m = lib(), _marshal or marshal()
+    _check(m.quantize(l.at_ts_quantize_fp8, x, fmt, q, q_scales, qt, qt_scales, stream), "ts_quantize_fp8")
+
+
+def ts_matmul_workspace_bytes(M: int, N: int, K: int) -> int:
+    b = C.c_int64(0)
+    _check(lib().ts_matmul_workspace_bytes(M, N, K, C.byref(b)), "ts_matmul_workspace_bytes")
+    return b.value
+
+
+def ts_matmul_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor, K: int, out: torch.Tensor,
+                  c_in: Optional[torch.Tensor] = None, stream=None) -> None:
+    """out = c_in + A B^T; a, b: codes as float8_e4m3fn or float8_e5m2, out [M, N] float32 or bfloat16."""
+    l, m = lib(), _marshal or marshal()
+    _check(m.matmul(l.at_ts_matmul_fp8, a, a_scales, b, b_scales, K, out, c_in, stream), "ts_matmul_fp8")
 
 
 def ts_fusion_place(capacity_bytes: int, used_bytes: int, d: int, V: int, out_dtype: int = TS_OUT_FP32):

@@ -332,12 +332,287 @@ PyObject* accumulate(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     });
 }
 
+// ---- dropout, lookup, products in 8 bits: all tensors of a call are on one GPU, the current one
+struct Device {
+    int index = -1;
+
+    void hold(const at::Tensor& t)
+    {
+        require(t.is_cuda() && t.is_contiguous());
+        if (index < 0) index = (int)t.get_device();
+        require(index == (int)t.get_device());
+    }
+    // stream (None: PyTorch's current one), which is this GPU's
+    void* stream(PyObject* o) const
+    {
+        PyObject* const now = PyObject_CallNoArgs(g_current_device);
+        if (!now) throw Failed();
+        const long current = PyLong_AsLong(now);
+        Py_DECREF(now);
+        if (current == -1 && PyErr_Occurred()) throw Failed();
+        require((int)current == index);
+        if (o != Py_None) {
+            PyObject* const its = PyObject_GetAttrString(o, "device_index");
+            if (!its) throw Failed();
+            const long d = PyLong_AsLong(its);
+            Py_DECREF(its);
+            if (d == -1 && PyErr_Occurred()) throw Failed();
+            require((int)d == index);
+        }
+        return stream_of(o);
+    }
+};
+
+// TS_ROW_* of a tensor (TS_OUT_* has the same numbers): float32, bfloat16 or 16-bit integers that hold its bits.
+int32_t value_type(const at::Tensor& t)
+{
+    const auto s = t.scalar_type();
+    require(s == at::kFloat || s == at::kBFloat16 || s == at::kShort || s == at::kUInt16);
+    return s == at::kFloat ? TS_ROW_FP32 : TS_ROW_BF16;
+}
+
+const int32_t* index_list(PyObject* o, Device& on, int64_t* n)
+{
+    const at::Tensor& t = tensor(o);
+    on.hold(t);
+    require(t.scalar_type() == at::kInt && t.dim() == 1);
+    *n = t.numel();
+    return static_cast<const int32_t*>(t.data_ptr());
+}
+
+// A matrix of `rows` rows (-1: any number) and `cols` columns (-1: any number, which it then is).
+const at::Tensor& matrix(PyObject* o, Device& on, int64_t rows, int64_t cols)
+{
+    const at::Tensor& t = tensor(o);
+    on.hold(t);
+    require(t.dim() == 2 && (rows < 0 || t.size(0) == rows) && (cols < 0 || t.size(1) == cols));
+    return t;
+}
+
+int32_t size32(int64_t n)
+{
+    require(n == (int32_t)n);
+    return (int32_t)n;
+}
+
+PyObject* attribute(PyObject* o, const char* name)
+{
+    PyObject* const v = PyObject_GetAttrString(o, name);
+    if (!v) throw Failed();
+    return v;
+}
+
+uint64_t word_attribute(PyObject* o, const char* name)
+{
+    PyObject* const v = attribute(o, name);
+    const unsigned long long x = PyLong_AsUnsignedLongLong(v);
+    Py_DECREF(v);
+    if (x == (unsigned long long)-1 && PyErr_Occurred()) throw Failed();
+    return x;
+}
+
+// The binding's DropoutMask: p, seed, offset, step (None, or a tensor of one int64 on the call's GPU).
+ts_dropout_mask mask_of(PyObject* o, Device& on)
+{
+    ts_dropout_mask m{};
+    m.seed = word_attribute(o, "seed");
+    m.offset = word_attribute(o, "offset");
+    PyObject* const p = attribute(o, "p");
+    const double x = PyFloat_AsDouble(p);
+    Py_DECREF(p);
+    if (x == -1.0 && PyErr_Occurred()) throw Failed();
+    m.p = (float)x;
+    PyObject* const step = attribute(o, "step");
+    try {
+        if (step != Py_None) {
+            const at::Tensor& t = tensor(step);
+            on.hold(t);
+            require(t.numel() == 1 && t.scalar_type() == at::kLong);
+            m.step = static_cast<const uint64_t*>(t.data_ptr());
+        }
+    } catch (...) {
+        Py_DECREF(step);
+        throw;
+    }
+    Py_DECREF(step);        // (the mask holds it)
+    return m;
+}
+
+double number(PyObject* o)
+{
+    const double x = PyFloat_AsDouble(o);
+    if (x == -1.0 && PyErr_Occurred()) throw Failed();
+    return x;
+}
+
+// dropout(entry, x, mask, out, add, stream)
+PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    return guarded(nargs, 6, [&] {
+        const auto fn = reinterpret_cast<decltype(&ts_dropout)>(address(a[0]));
+        Device on;
+        const at::Tensor& x = matrix(a[1], on, -1, -1);
+        const int64_t n = x.size(0), d = x.size(1);
+        const at::Tensor& out = matrix(a[3], on, n, d);
+        const void* add = nullptr;
+        if (a[4] != Py_None) {
+            const at::Tensor& t = matrix(a[4], on, n, d);
+            require(value_type(t) == value_type(x));
+            add = t.data_ptr();
+        }
+        const int32_t type = value_type(x);
+        require(value_type(out) == type);
+        const ts_dropout_mask m = mask_of(a[2], on);
+        void* const stream = on.stream(a[5]);
+        const void* const from = x.data_ptr();
+        void* const to = out.data_ptr();
+        const int32_t width = size32(d);
+        return status([&] { return fn(from, add, n, width, type, &m, to, stream); });
+    });
+}
+
+// lookup(entry, ids, weight, scale, mask, out, pos, pos_ids, stream)
+PyObject* lookup(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    return guarded(nargs, 9, [&] {
+        const auto fn = reinterpret_cast<decltype(&ts_lookup_dropout)>(address(a[0]));
+        Device on;
+        int64_t n, n_at = 0;
+        const int32_t *ids = index_list(a[1], on, &n), *pos_ids = nullptr;
+        const at::Tensor& weight = matrix(a[2], on, -1, -1);
+        const int32_t V = size32(weight.size(0)), d = size32(weight.size(1)), type = value_type(weight);
+        const at::Tensor& out = matrix(a[5], on, n, d);
+        const int32_t out_type = value_type(out);
+        const void* pos = nullptr;
+        int32_t n_pos = 0;
+        require((a[6] == Py_None) == (a[7] == Py_None));
+        if (a[6] != Py_None) {
+            const at::Tensor& t = matrix(a[6], on, -1, d);
+            require(value_type(t) == type);
+            pos = t.data_ptr();
+            n_pos = size32(t.size(0));
+            pos_ids = index_list(a[7], on, &n_at);
+            require(n_at == n);
+        }
+        const float scale = (float)number(a[3]);
+        const ts_dropout_mask m = mask_of(a[4], on);
+        void* const stream = on.stream(a[8]);
+        const void* const from = weight.data_ptr();
+        void* const to = out.data_ptr();
+        return status([&] { return fn(ids, n, from, type, d, V, scale, pos, pos_ids, n_pos, &m, to, out_type, stream); });
+    });
+}
+
+// densify_dropout(entry, ids, rows, d, V, scale, mask, dense_in, dense_out, stream)
+PyObject* densify_dropout(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    return guarded(nargs, 10, [&] {
+        const auto fn = reinterpret_cast<decltype(&ts_densify_dropout)>(address(a[0]));
+        Device on;
+        const int32_t d = integer32(a[3]), V = integer32(a[4]);
+        int64_t n;
+        const int32_t* const ids = index_list(a[1], on, &n);
+        const at::Tensor& rows = matrix(a[2], on, n, d);
+        const int32_t type = value_type(rows);
+        const at::Tensor& out = matrix(a[8], on, V, d);
+        require(out.scalar_type() == at::kFloat);
+        const float* in = nullptr;
+        if (a[7] != Py_None) {
+            const at::Tensor& t = matrix(a[7], on, V, d);
+            require(t.scalar_type() == at::kFloat);
+            in = static_cast<const float*>(t.data_ptr());
+        }
+        const float scale = (float)number(a[5]);
+        const ts_dropout_mask m = mask_of(a[6], on);
+        void* const stream = on.stream(a[9]);
+        const void* const from = rows.data_ptr();
+        float* const to = static_cast<float*>(out.data_ptr());
+        return status([&] { return fn(ids, from, n, type, d, V, scale, &m, in, to, stream); });
+    });
+}
+
+// Rows of codes (uint8, or PyTorch's type of the format) and of scales (uint8) for K columns, as ts_fp8_layout has them.
+int64_t code_row(int64_t K) { return (K + TS_FP8_BLOCK - 1) / TS_FP8_BLOCK * TS_FP8_BLOCK; }
+int64_t scale_row(int64_t K) { return ((K + TS_FP8_BLOCK - 1) / TS_FP8_BLOCK + 3) / 4 * 4; }
+
+uint8_t* scale_bytes(PyObject* o, Device& on, int64_t rows, int64_t K)
+{
+    const at::Tensor& t = matrix(o, on, rows, scale_row(K));
+    require(t.scalar_type() == at::kByte);
+    return static_cast<uint8_t*>(t.data_ptr());
+}
+
+int32_t format_of(const at::Tensor& t)
+{
+    const auto s = t.scalar_type();
+    require(s == at::kFloat8_e4m3fn || s == at::kFloat8_e5m2);
+    return s == at::kFloat8_e4m3fn ? TS_FP8_E4M3 : TS_FP8_E5M2;
+}
+
+// quantize(entry, x, format, q, q_scales, qt, qt_scales, stream)
+PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    return guarded(nargs, 8, [&] {
+        const auto fn = reinterpret_cast<decltype(&ts_quantize_fp8)>(address(a[0]));
+        Device on;
+        const at::Tensor& x = matrix(a[1], on, -1, -1);
+        const int64_t rows = x.size(0), cols = x.size(1);
+        const int32_t type = value_type(x), format = integer32(a[2]);
+        uint8_t *codes[2] = {nullptr, nullptr}, *scales[2] = {nullptr, nullptr};
+        for (int t = 0; t < 2; ++t) {
+            const int64_t r = t ? cols : rows, k = t ? rows : cols;
+            require((a[3 + 2 * t] == Py_None) == (a[4 + 2 * t] == Py_None));
+            if (a[3 + 2 * t] == Py_None) continue;
+            const at::Tensor& q = matrix(a[3 + 2 * t], on, r, code_row(k));
+            require(q.scalar_type() == at::kByte || format_of(q) == format);
+            codes[t] = static_cast<uint8_t*>(q.data_ptr());
+            scales[t] = scale_bytes(a[4 + 2 * t], on, r, k);
+        }
+        void* const stream = on.stream(a[7]);
+        const void* const from = x.data_ptr();
+        // (an empty tensor has no address: there is nothing to write then)
+        if (rows == 0 || cols == 0) return PyLong_FromLong(TS_OK);
+        return status([&] { return fn(from, type, rows, cols, format, codes[0], scales[0], codes[1], scales[1], stream); });
+    });
+}
+
+// matmul(entry, a, a_scales, b, b_scales, K, out, c_in, stream)
+PyObject* matmul(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    return guarded(nargs, 9, [&] {
+        const auto fn = reinterpret_cast<decltype(&ts_matmul_fp8)>(address(a[0]));
+        Device on;
+        const int64_t K = integer(a[5]);
+        require(K >= 0 && K == (int32_t)K);
+        const at::Tensor& out = matrix(a[6], on, -1, -1);
+        const int64_t M = out.size(0), N = out.size(1);
+        const at::Tensor &u = matrix(a[1], on, M, code_row(K)), &v = matrix(a[3], on, N, code_row(K));
+        const int32_t fu = format_of(u), fv = format_of(v), out_type = value_type(out);
+        const uint8_t *su = scale_bytes(a[2], on, M, K), *sv = scale_bytes(a[4], on, N, K);
+        const float* in = nullptr;
+        if (a[7] != Py_None) {
+            const at::Tensor& t = matrix(a[7], on, M, N);
+            require(t.scalar_type() == at::kFloat);
+            in = static_cast<const float*>(t.data_ptr());
+        }
+        void* const stream = on.stream(a[8]);
+        const uint8_t *pu = static_cast<const uint8_t*>(u.data_ptr()), *pv = static_cast<const uint8_t*>(v.data_ptr());
+        void* const to = out.data_ptr();
+        return status([&] { return fn(pu, su, fu, pv, sv, fv, M, N, K, in, to, out_type, stream); });
+    });
+}
+
 PyMethodDef methods[] = {
     {"densify", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(densify)), METH_FASTCALL, nullptr},
     {"multi", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(multi)), METH_FASTCALL, nullptr},
     {"scaled", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(scaled)), METH_FASTCALL, nullptr},
     {"range", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(range)), METH_FASTCALL, nullptr},
     {"accumulate", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(accumulate)), METH_FASTCALL, nullptr},
+    {"dropout", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(dropout)), METH_FASTCALL, nullptr},
+    {"lookup", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(lookup)), METH_FASTCALL, nullptr},
+    {"densify_dropout", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(densify_dropout)), METH_FASTCALL, nullptr},
+    {"quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(quantize)), METH_FASTCALL, nullptr},
+    {"matmul", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(matmul)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 

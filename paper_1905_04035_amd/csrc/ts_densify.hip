@@ -54,8 +54,10 @@
 #include <string.h>
 #include <type_traits>
 
+#include "philox.h"
 #include "ts_densify.h"
 #include "ts_densify_tools.h"
+#include "ts_workspace.h"
 
 // Built-in workspace of ts_densify_static, the entry point for callers that cannot allocate.
 // One copy per GPU, held from the moment the library is loaded on it until the process
@@ -245,7 +247,32 @@ __device__ __forceinline__ void store_f4_stream(float* p, f4 v)
 // (untouched rows are bit copies of dense_in).  EPI_SCALE: every element multiplied by one
 // fp32 factor (an average over k contributions is scale = 1/k).  EPI_SCALE_BF16: the same,
 // then rounded to bf16 (nearest, ties to even), which halves the bytes written.
-enum { EPI_NONE = 0, EPI_SCALE = 1, EPI_SCALE_BF16 = 2 };
+// EPI_DROP: stored as with EPI_NONE; it is the value rows that are not taken as they are (drop_rows).
+enum { EPI_NONE = 0, EPI_SCALE = 1, EPI_SCALE_BF16 = 2, EPI_DROP = 3 };
+
+// The value rows of ts_densify_dropout: where they begin, and the mask that goes with them.
+struct Drop {
+    uint64_t rows;
+    ts_mask::Mask mask;
+};
+
+template <int EPI>
+__device__ __forceinline__ uint64_t drop_offset(const Drop& p)
+{
+    return EPI == EPI_DROP ? ts_mask::offset_now(p.mask) : 0ull;
+}
+
+// The mask's share of a lane's columns col .. col + 4 * NV - 1 of the value row at row_addr: the place of four elements among the
+// call's follows from their address.
+template <typename RowT, int EPI, int NV>
+__device__ __forceinline__ void drop_rows(f4 (&r)[NV], uint64_t row_addr, int col, uint64_t offset, const Drop& p)
+{
+    if constexpr (EPI == EPI_DROP) {
+        const uint64_t group = ((row_addr - p.rows) / sizeof(RowT) + (uint64_t)col) >> 2;
+#pragma unroll
+        for (int q = 0; q < NV; ++q) r[q] = ts_mask::apply<false>(r[q], (f4)(0.0f), group + q, offset, p.mask);
+    }
+}
 
 __device__ __forceinline__ uint32_t bf16_rne(float x)
 {
@@ -258,7 +285,7 @@ __device__ __forceinline__ uint32_t bf16_rne(float x)
 template <int EPI>
 __device__ __forceinline__ void store_out(void* out, size_t idx, f4 v, float scale)
 {
-    if (EPI == EPI_NONE) {
+    if (EPI == EPI_NONE || EPI == EPI_DROP) {
         store_f4_stream(reinterpret_cast<float*>(out) + idx, v);
     } else if (EPI == EPI_SCALE) {
         store_f4_stream(reinterpret_cast<float*>(out) + idx, v * scale);
@@ -307,7 +334,7 @@ __device__ __forceinline__ void copy_flat(const float* dense_in, void* dense_out
     // multiply placed between two stores makes the compiler wait for the earlier store
     // (the empty asm statements keep it from moving the arithmetic down to the stores).
     u2 packed[U];
-    if constexpr (EPI != EPI_NONE) {
+    if constexpr (EPI != EPI_NONE && EPI != EPI_DROP) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             x[u] = x[u] * scale;
@@ -350,7 +377,7 @@ __device__ __forceinline__ void copy_chunk(const float* dense_in, void* dense_ou
     }
     // every value is transformed before the first store is issued, as in copy_flat
     u2 packed[4];
-    if constexpr (EPI != EPI_NONE) {
+    if constexpr (EPI != EPI_NONE && EPI != EPI_DROP) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             x[u] = x[u] * scale;
@@ -1070,6 +1097,7 @@ struct ReduceParams {
     int32_t logC, logG;         // log2 C; log2 of the sorted positions of a group of pieces
     uint32_t row_magic;         // ceil(2^20 / d), where row_chunks < 0
     int32_t part_owned;         // the call owns a range of the ids: most groups of pieces may be empty
+    Drop drop;                  // EPI_DROP
 };
 
 // Pieces per work-group of the reduce kernel, one per wavefront: 64 sorted positions with pieces of 8
@@ -1238,6 +1266,7 @@ __device__ __forceinline__ void short_row(const ReduceParams& p, int v, int c0, 
     if (early) load_dense(c0);
     const int c = p.count[v];
     if (c > p.short_max || (c == 0 && !copy)) return;
+    const uint64_t mask_offset = drop_offset<EPI>(p.drop);
     uint64_t addr = 0;
     if (lane < c) addr = p.sorted[p.row_start[v] + lane].row_addr;
     if (!early) load_dense(c0);
@@ -1264,6 +1293,7 @@ __device__ __forceinline__ void short_row(const ReduceParams& p, int v, int c0, 
                     for (int u = 0; u < 4; ++u) {
                         f4 r[1];
                         RowLoad<RowT, 1>::widen(raw[t][u], r);
+                        drop_rows<RowT, EPI>(r, bcast64(addr, j0 + t), min(c0 + u * kColBlock + lane * 4, d - 4), mask_offset, p.drop);
                         acc[u] = acc[u] + r[0];
                     }
                 }
@@ -1340,6 +1370,7 @@ __device__ __forceinline__ void group_wave(const ReduceParams& p, int kg, int cb
         any = any || L[w] != 0;
     }
     if (!any) return;
+    const uint64_t mask_offset = drop_offset<EPI>(p.drop);
     const uint64_t PS = ballot64((lane & (C - 1)) == 0);            // first and last position of a piece
     const uint64_t PE = ballot64((lane & (C - 1)) == C - 1);        // (C divides 64)
 
@@ -1404,6 +1435,7 @@ __device__ __forceinline__ void group_wave(const ReduceParams& p, int kg, int cb
                     if (fresh) segfirst = rs || (w == 0 && j == 0);
                     f4 r[NV];
                     RowLoad<RowT, NV>::widen(raw[u], r);
+                    drop_rows<RowT, EPI>(r, bcast64(addr[w], j), col, mask_offset, p.drop);
 #pragma unroll
                     for (int q = 0; q < NV; ++q) acc[q] = (fresh ? (f4)(0.0f) : acc[q]) + r[q];
                     if (re || pe) {
@@ -1587,6 +1619,7 @@ __global__ __launch_bounds__(64 * GP) void reduce_kernel(ReduceParams p)
 
     if (A != 0) {
         typedef typename RowLoad<RowT, NV>::Raw Raw;
+        const uint64_t mask_offset = drop_offset<EPI>(p.drop);
         f4 acc[NV];
 #pragma unroll
         for (int q = 0; q < NV; ++q) acc[q] = (f4)(0.0f);
@@ -1633,6 +1666,7 @@ __global__ __launch_bounds__(64 * GP) void reduce_kernel(ReduceParams p)
                         const bool fresh = (F >> j) & 1ull;
                         f4 r[NV];
                         RowLoad<RowT, NV>::widen(raw[u], r);
+                        drop_rows<RowT, EPI>(r, bcast64(addr, j), col, mask_offset, p.drop);
 #pragma unroll
                         for (int q = 0; q < NV; ++q) acc[q] = (fresh ? (f4)(0.0f) : acc[q]) + r[q];
                         if ((Lm >> j) & 1ull) {
@@ -1772,6 +1806,7 @@ struct SmallParams {
     void* dense_out;
     int32_t copy_untouched;
     float scale;
+    Drop drop;                  // EPI_DROP
 };
 
 // LDS: the counts per (wavefront, id), per id its pairs and first position, per sorted pair the address of its value row
@@ -1916,6 +1951,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void small_kernel(SmallParams p, 
     __syncthreads();
 
     const uint32_t off = (uint32_t)colr * (uint32_t)sizeof(RowT);
+    const uint64_t mask_offset = drop_offset<EPI>(p.drop);
     const auto load_pair = [&](int lp) {
         typedef const Raw __attribute__((address_space(1))) * global_raw;
         return __builtin_nontemporal_load(reinterpret_cast<global_raw>(row_addr[lp] + off));
@@ -1959,6 +1995,10 @@ __global__ __launch_bounds__(64 * kSmallWaves) void small_kernel(SmallParams p, 
                 for (int u = 0; u < 8; ++u) {
                     f4 x[1];
                     RowLoad<RowT, 1>::widen(raw[u], x);
+                    if constexpr (EPI == EPI_DROP) {
+                        if (at + u < end0 || (at + u >= begin1 && at + u < end))
+                            drop_rows<RowT, EPI>(x, row_addr[at + u - (int)base], colr, mask_offset, p.drop);
+                    }
                     if (at + u < end0) acc[0] = acc[0] + x[0];
                     if (at + u >= begin1 && at + u < end) acc[1] = acc[1] + x[0];
                 }
@@ -2029,6 +2069,9 @@ __global__ __launch_bounds__(64 * kSmallWaves) void small_kernel(SmallParams p, 
                         for (int u = 0; u < 8; ++u) {
                             f4 x[1];
                             RowLoad<RowT, 1>::widen(raw[u], x);
+                            if constexpr (EPI == EPI_DROP) {
+                                if (j0 + u < c) drop_rows<RowT, EPI>(x, row_addr[lp + j0 + u], colr, mask_offset, p.drop);
+                            }
                             if (j0 + u < c) acc[0] = acc[0] + x[0];
                         }
                     }
@@ -2416,11 +2459,17 @@ void launch_reduce(unsigned grid, bool wide, bool deep, int32_t row_dtype, hipSt
         launch_reduce_as<EPI, 0, 4, false>(grid, wide, row_dtype, stream, begin, end, rp);
 }
 
+// (the launches that do not touch value rows have no form of their own for EPI_DROP)
 #define TS_DISPATCH_EPI(epi, fn, ...)                              \
     do {                                                           \
-        if ((epi) == EPI_NONE) fn<EPI_NONE>(__VA_ARGS__);          \
+        if ((epi) == EPI_NONE || (epi) == EPI_DROP) fn<EPI_NONE>(__VA_ARGS__); \
         else if ((epi) == EPI_SCALE) fn<EPI_SCALE>(__VA_ARGS__);   \
         else fn<EPI_SCALE_BF16>(__VA_ARGS__);                      \
+    } while (0)
+#define TS_DISPATCH_ROWS(epi, fn, ...)                             \
+    do {                                                           \
+        if ((epi) == EPI_DROP) fn<EPI_DROP>(__VA_ARGS__);          \
+        else TS_DISPATCH_EPI(epi, fn, __VA_ARGS__);                \
     } while (0)
 
 void remember(const Plan& pl, void* ws, int32_t V, int32_t copied_beside, int32_t form)
@@ -2490,9 +2539,11 @@ void launch_small(unsigned grid, size_t lds, int32_t row_dtype, hipStream_t stre
 }
 
 int densify_small(const ShardTable& sh, Plan& pl, int32_t row_dtype, int32_t d, int32_t V, int32_t id_base, int32_t V_total,
-                  const float* dense_in, void* dense_out, int epi, float scale, hipStream_t stream, char* ws, bool in_place, bool wide)
+                  const float* dense_in, void* dense_out, int epi, float scale, hipStream_t stream, char* ws, bool in_place, bool wide,
+                  const Drop& drop)
 {
     SmallParams q;
+    q.drop = drop;
     q.n = sh.off[sh.k];
     q.V = V;
     q.id_base = id_base;
@@ -2523,11 +2574,11 @@ int densify_small(const ShardTable& sh, Plan& pl, int32_t row_dtype, int32_t d, 
     q.n_bad = (int32_t*)(ws + pl.off_nbad);
     q.dense_in = dense_in;
     q.dense_out = dense_out;
-    q.copy_untouched = !(in_place && epi == EPI_NONE);
+    q.copy_untouched = !(in_place && (epi == EPI_NONE || epi == EPI_DROP));
     q.scale = scale;
     const bool prof = g_prof_used < g_prof_cap;
     hipEvent_t ev_begin = prof ? g_ev[2 * g_prof_used] : nullptr, ev_end = prof ? g_ev[2 * g_prof_used + 1] : nullptr;
-    TS_DISPATCH_EPI(epi, launch_small, (unsigned)(q.stride * ncb), small_lds(q.n, q.part, q.lanes), row_dtype, stream, ev_begin, ev_end, q, sh);
+    TS_DISPATCH_ROWS(epi, launch_small, (unsigned)(q.stride * ncb), small_lds(q.n, q.part, q.lanes), row_dtype, stream, ev_begin, ev_end, q, sh);
     if (prof) ++g_prof_used;
     if (hipGetLastError() != hipSuccess) return TS_ERR_HIP;
     pl.part = q.part;
@@ -2538,7 +2589,7 @@ int densify_small(const ShardTable& sh, Plan& pl, int32_t row_dtype, int32_t d, 
 // V rows are produced: ids id_base .. id_base + V - 1 of a vocabulary of V_total ids.
 int densify_impl(const ShardTable& sh, int64_t n, int32_t row_dtype, int32_t d, int32_t V, int32_t id_base,
                  int32_t V_total, const float* dense_in, void* dense_out, int epi, float scale, void* stream_v,
-                 void* ws_v, int64_t ws_bytes)
+                 void* ws_v, int64_t ws_bytes, const Drop& drop)
 {
     const bool wide = row_dtype == TS_ROW_BF16 && (d % 8) == 0;     // 16-byte loads of bf16 rows
     const bool in_place = (const void*)dense_in == (const void*)dense_out;
@@ -2562,7 +2613,8 @@ int densify_impl(const ShardTable& sh, int64_t n, int32_t row_dtype, int32_t d, 
     hipStream_t stream = (hipStream_t)stream_v;
     char* ws = (char*)ws_v;
 
-    if (small_call(n, d, V)) return densify_small(sh, pl, row_dtype, d, V, id_base, V_total, dense_in, dense_out, epi, scale, stream, ws, in_place, wide);
+    if (small_call(n, d, V)) return densify_small(sh, pl, row_dtype, d, V, id_base, V_total, dense_in, dense_out, epi, scale, stream, ws, in_place, wide,
+                                               drop);
 
     SortParams sp;
     sp.n = (int32_t)n;
@@ -2588,7 +2640,7 @@ int densify_impl(const ShardTable& sh, int64_t n, int32_t row_dtype, int32_t d, 
     // In place, the plain path leaves untouched rows alone.  With an epilogue they still have
     // to be scaled, by the item that reads them; only the copy made before the pairs are
     // sorted must go, because the reduce kernel would read scaled values.
-    const bool skip_untouched = in_place && epi == EPI_NONE;
+    const bool skip_untouched = in_place && (epi == EPI_NONE || epi == EPI_DROP);
     // Rows copied by the sort launches: about as many bytes as HBM moves while a sort runs.  One slice: 32 MiB plus 1 MiB
     // per 1024 pairs up to 16384 pairs, 1.25 MiB per 1024 pairs beyond (the wavefronts then walk their shares in several
     // rounds; 2.5 MiB copies too many rows that receive pairs: V = 32768, d = 1024, 40000 pairs 84.9 us with 1.25, 86.5 with
@@ -2696,6 +2748,7 @@ int densify_impl(const ShardTable& sh, int64_t n, int32_t row_dtype, int32_t d, 
     rp.copy_row0 = copy_done;
     rp.copy_untouched = skip_untouched ? 0 : 1;
     rp.row_start = sp.row_start;
+    rp.drop = drop;
     rp.short_max = by_row ? pl.C : 0;
     // with pieces of at most 16 positions, the long rows by wavefronts that work alone, four groups
     // of pieces to a work-group
@@ -2714,7 +2767,7 @@ int densify_impl(const ShardTable& sh, int64_t n, int32_t row_dtype, int32_t d, 
     const bool prof = g_prof_used < g_prof_cap && rgrid > 0;
     hipEvent_t ev_begin = prof ? g_ev[2 * g_prof_used] : nullptr;
     hipEvent_t ev_end = prof ? g_ev[2 * g_prof_used + 1] : nullptr;
-    if (rgrid > 0) TS_DISPATCH_EPI(epi, launch_reduce, rgrid, wide, deep, row_dtype, stream, ev_begin, ev_end, rp);
+    if (rgrid > 0) TS_DISPATCH_ROWS(epi, launch_reduce, rgrid, wide, deep, row_dtype, stream, ev_begin, ev_end, rp);
     if (prof) ++g_prof_used;
     if (hipGetLastError() != hipSuccess) return TS_ERR_HIP;
 
@@ -2737,7 +2790,7 @@ int validate_common(int64_t n_total, int32_t d, int32_t V, const float* dense_in
 int densify_shards(const int32_t* const* ids_k, const void* const* rows_k, const int64_t* n_k, int32_t k,
                    int32_t row_dtype, int32_t d, int32_t V, const float* dense_in, void* dense_out, int epi,
                    float scale, void* stream, int32_t v_begin = 0, int32_t v_end = -1, void* ws = nullptr,
-                   int64_t ws_bytes = -1)
+                   int64_t ws_bytes = -1, const ts_mask::Mask* mask = nullptr)
 {
     if (ws_bytes < 0) {         // the bound workspace
         ws = g_ws;
@@ -2770,11 +2823,29 @@ int densify_shards(const int32_t* const* ids_k, const void* const* rows_k, const
         off += n_k[j];
     }
     for (int j = k; j <= TS_MAX_SHARDS; ++j) sh.off[j] = (int32_t)off;
+    Drop drop;
+    memset(&drop, 0, sizeof drop);
+    if (mask) {                 // one shard
+        drop.rows = (uint64_t)(uintptr_t)rows_k[0];
+        drop.mask = *mask;
+    }
     return densify_impl(sh, n_total, row_dtype, d, v_end - v_begin, v_begin, V, dense_in, dense_out, epi, scale, stream,
-                        ws, ws_bytes);
+                        ws, ws_bytes, drop);
 }
 
 }  // namespace
+
+namespace ts_workspace {
+
+int take(int64_t bytes, void** ws)
+{
+    if (!g_ws || bytes > g_ws_bytes) return TS_ERR_WORKSPACE;
+    if (g_last_ws == g_ws) g_have_last = false;         // the views of the last call end here
+    *ws = g_ws;
+    return TS_OK;
+}
+
+}  // namespace ts_workspace
 
 // ------------------------------------------------------------------ C ABI
 extern "C" {
@@ -2835,6 +2906,15 @@ int ts_densify_range(const int32_t* const* ids_k, const void* const* rows_k, con
     if (v_end < 0) return TS_ERR_SHAPE;
     return densify_shards(ids_k, rows_k, n_k, k, row_dtype, d, V, dense_in, dense_out, EPI_NONE, 1.0f, stream,
                           v_begin, v_end);
+}
+
+int ts_densify_dropout(const int32_t* ids, const void* rows, int64_t n, int32_t row_dtype, int32_t d, int32_t V, float scale,
+                       const ts_dropout_mask* mask, const float* dense_in, float* dense_out, void* stream)
+{
+    ts_mask::Mask m;
+    const int rc = ts_mask::make(mask, scale, &m);
+    if (rc != TS_OK) return rc;
+    return densify_shards(&ids, &rows, &n, 1, row_dtype, d, V, dense_in, dense_out, EPI_DROP, 1.0f, stream, 0, -1, nullptr, -1, &m);
 }
 
 int ts_fusion_place(int64_t capacity_bytes, int64_t used_bytes, int32_t d, int32_t V, int32_t out_dtype,

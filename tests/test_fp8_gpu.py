@@ -1,0 +1,286 @@
+"""8-bit codes with a scale for each block of 128, and products of them, on the GPU against the checker.
+
+Codes and scales are compared bit for bit.  Products of two codes have at most 8 significant bits and are exact in fp32, so an
+element's error comes from its additions alone: at most K rounded ones (and the c_in), each off by at most 2^-23 of
+a partial sum even if a unit cuts instead of rounding, so by at most (K + 1) 2^-23 of the sum of the terms' magnitudes; where
+all partial sums are whole numbers below 2^24 there is no error at all.  A bf16 result is made by instructions that cut, in
+each group of eight products, what lies below 2^-13 of the largest one's power of two: at most 2^-13 of the largest for each of the
+other seven, so less than 7 * 2^-13 of the group's magnitudes, before its own rounding of 2^-8."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as op
+from paper_1905_04035_amd import binding as ts
+from tests.parity import DEV
+
+pytestmark = pytest.mark.gpu
+
+FP32, BF16 = torch.float32, torch.bfloat16
+E4M3, E5M2 = ts.TS_FP8_E4M3, ts.TS_FP8_E5M2
+
+
+def same_codes(q, want, fmt):
+    got = q.view(torch.uint8).cpu().numpy()
+    nan = np.isnan(op.decode(fmt)[want])
+    assert np.array_equal(np.isnan(op.decode(fmt)[got]), nan) and np.array_equal(got[~nan], want[~nan])
+
+
+def quantized(x, fmt, ways="both"):
+    """(q, scales, qt, scales of it) on the GPU, every byte of them written."""
+    rows, cols = x.shape
+    out = []
+    for r, k in ((rows, cols), (cols, rows)):
+        q, s = ts.fp8_empty(r, k, fmt)
+        q.view(torch.uint8).fill_(0x55)
+        s.fill_(0x55)
+        out += [q, s]
+    a = out[:2] if ways != "turned" else [None, None]
+    b = out[2:] if ways != "rows" else [None, None]
+    ts.ts_quantize_fp8(x.to(DEV), fmt, *a, *b)
+    return a + b
+
+
+SIZES = [(1, 1), (1, 64), (1, 1024), (3, 130), (127, 128), (128, 127), (129, 257), (64, 1000), (1021, 512), (300, 700), (5, 4100)]
+
+
+@pytest.mark.parametrize("rows,cols", SIZES)
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("fmt", [E4M3, E5M2])
+def test_quantize(rows, cols, dtype, fmt):
+    g = torch.Generator().manual_seed(rows * 5000 + cols)
+    x = (torch.randn(rows, cols, generator=g) * torch.exp2(torch.randn(rows, 1, generator=g) * 8)).to(dtype)
+    x[torch.rand(rows, cols, generator=g) < 0.05] = 0.0
+    h = x.float().numpy()
+    for ways in ("rows", "turned", "both"):
+        q, s, qt, st = quantized(x, fmt, ways)
+        for codes, scales, of in ((q, s, h), (qt, st, h.T)):
+            if codes is not None:
+                want, want_scales = op.quantize(of, fmt)
+                assert np.array_equal(scales.cpu().numpy(), want_scales)
+                same_codes(codes, want, fmt)
+
+
+@pytest.mark.parametrize("fmt", [E4M3, E5M2])
+def test_quantize_special_values(fmt):
+    top = op.FORMATS[fmt][2]
+    x = np.zeros((12, 256), dtype=np.float32)
+    x[0, :128] = np.nan                                              # nothing finite
+    x[1, 5:8] = np.nan, np.inf, -np.inf
+    x[1, 9] = 3.0
+    x[2, 0], x[2, 1] = 3.4028234e38, -3.4028234e38
+    x[3, 0], x[3, 1] = 2.0 ** -149, -2.0 ** -140
+    x[4, 0], x[4, 1] = 2.0 ** -126, 2.0 ** -135
+    x[5, 0], x[5, 1] = top, -0.0
+    x[6, 0] = np.nextafter(np.float32(top), np.float32(np.inf))
+    x[7] = np.ldexp(1.0, -np.arange(256) % 40)                       # down to what underflows, ties on the way
+    x[8] = 1.0 + np.arange(256) / 64.0
+    x[9] = -(1.0 + np.arange(256) / 64.0) * 2.0 ** -14
+    x[10, 200] = 1.0                                                 # a block of zeros before
+    q, s, qt, st = quantized(torch.from_numpy(x), fmt)
+    for codes, scales, of in ((q, s, x), (qt, st, x.T)):
+        want, want_scales = op.quantize(of, fmt)
+        assert np.array_equal(scales.cpu().numpy(), want_scales)
+        same_codes(codes, want, fmt)
+
+
+def operand(rows, K, fmt, kind, seed):
+    """(codes, scales) as numpy arrays."""
+    rng = np.random.default_rng(seed)
+    blocks = -(-K // 128)
+    codes = np.zeros((rows, blocks * 128), dtype=np.uint8)
+    scales = np.zeros((rows, -(-blocks // 4) * 4), dtype=np.uint8)
+    if kind == "whole":                                              # whole numbers to 4, scales of 1, 2, 4
+        codes[:, :K] = op.encode(rng.integers(-4, 5, (rows, K)), fmt)
+        scales[:, :blocks] = rng.integers(127, 130, (rows, blocks))
+    else:
+        codes[:, :K] = op.encode(np.clip(rng.standard_normal((rows, K)) * 40, -400, 400), fmt)
+        scales[:, :blocks] = rng.integers(100, 150, (rows, blocks))
+    return codes, scales
+
+
+def on_gpu(codes, scales, fmt):
+    return (torch.from_numpy(codes).to(DEV).view(torch.float8_e5m2 if fmt else torch.float8_e4m3fn), torch.from_numpy(scales).to(DEV))
+
+
+def bind(M, N, K):
+    size = ts.ts_matmul_workspace_bytes(M, N, K)
+    ws = torch.empty(max(size, 256), dtype=torch.uint8, device=DEV)
+    ws.fill_(0xFF)                                                   # NaNs
+    ts.ts_bind_workspace(ws)
+    return ws
+
+
+def product(a, sa, fa, b, sb, fb, K, dtype, c_in=None, in_place=False):
+    M, N = len(a), len(b)
+    whole = torch.full((M * N + 64,), -7.0, dtype=dtype, device=DEV)
+    out = whole[:M * N].view(M, N)
+    if c_in is not None:
+        c_in = torch.from_numpy(c_in).to(DEV)
+        if in_place:
+            out.copy_(c_in)
+            c_in = out
+    ws = bind(M, N, K)
+    try:
+        ts.ts_matmul_fp8(*on_gpu(a, sa, fa), *on_gpu(b, sb, fb), K, out, c_in)
+        torch.cuda.synchronize()
+    finally:
+        ts.ts_bind_workspace(None)
+        del ws
+    assert (whole[M * N:] == -7).all()                               # nothing behind the result
+    return out.float().cpu().numpy().astype(np.float64)
+
+
+# few rows, few columns, odd ones, tiles that end inside, one block and many, products that are split along K
+PRODUCTS = [(1, 1, 1), (1, 32768, 64), (1, 1000, 1024), (2, 130, 200), (7, 999, 300), (16, 512, 512), (17, 1001, 129), (33, 260, 4987),
+            (64, 1024, 8192), (100, 100, 100), (128, 128, 128), (129, 257, 385), (256, 512, 640), (257, 255, 1000), (300, 5000, 64),
+            (1000, 64, 2048), (1024, 1024, 1024), (2000, 1500, 257), (515, 4097, 512), (1, 16, 40000), (40, 48, 70000)]
+
+
+@pytest.mark.parametrize("M,N,K", PRODUCTS)
+def test_products_of_whole_numbers_are_exact(M, N, K):
+    a, sa = operand(M, K, E4M3, "whole", M + K)
+    b, sb = operand(N, K, E4M3, "whole", N + K + 1)
+    want, size = op.matmul(a, sa, 0, b, sb, 0)
+    assert size.max() < 2 ** 24 and np.array_equal(want, np.rint(want))
+    assert np.array_equal(product(a, sa, 0, b, sb, 0, K, FP32), want)
+
+
+@pytest.mark.parametrize("M,N,K", [s for s in PRODUCTS if s[0] * s[1] * s[2] < 3e8])
+@pytest.mark.parametrize("fa,fb", [(E4M3, E4M3), (E5M2, E4M3), (E4M3, E5M2), (E5M2, E5M2)])
+def test_products(M, N, K, fa, fb):
+    a, sa = operand(M, K, fa, "any", M + K)
+    b, sb = operand(N, K, fb, "any", N + K + 1)
+    want, size = op.matmul(a, sa, fa, b, sb, fb)
+    got = product(a, sa, fa, b, sb, fb, K, FP32)
+    tol = (K + 1) * 2.0 ** -23
+    assert (np.abs(got - want) <= tol * size).all()
+    low = product(a, sa, fa, b, sb, fb, K, BF16)
+    assert (np.abs(low - want) <= ((tol + 7 * 2.0 ** -13) * size) * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want)).all()
+    c_in = np.random.default_rng(9).standard_normal((M, N)).astype(np.float32) * np.float32(np.abs(want).mean() + 1)
+    for in_place in (False, True):
+        onto = product(a, sa, fa, b, sb, fb, K, FP32, c_in, in_place)
+        assert (np.abs(onto - want - c_in) <= tol * (size + np.abs(c_in))).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 40, 300), (200, 300, 500), (300, 64, 9000)])
+def test_the_same_bits_twice_and_on_another_stream(M, N, K):
+    a, b = operand(M, K, E4M3, "any", 1), operand(N, K, E4M3, "any", 2)
+    u, v = on_gpu(*a, 0), on_gpu(*b, 0)
+    ws = bind(M, N, K)
+    outs = [torch.empty(M, N, device=DEV) for _ in range(3)]
+    s = torch.cuda.Stream()
+    for i, out in enumerate(outs):
+        torch.cuda.synchronize()
+        ts.ts_matmul_fp8(*u, *v, K, out, stream=s if i == 2 else None)
+    torch.cuda.synchronize()
+    ts.ts_bind_workspace(None)
+    del ws
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+def test_nan_and_infinity_reach_their_row_or_column_alone():
+    M, N, K = 20, 36, 200
+    for fa, code in ((E4M3, 0x7F), (E5M2, 0x7C)):
+        a, sa = operand(M, K, fa, "any", 1)
+        b, sb = operand(N, K, E4M3, "any", 2)
+        a[3, 150] = code
+        got = product(a, sa, fa, b, sb, 0, K, FP32)
+        assert not np.isfinite(got[3]).any()
+        rest = np.delete(np.arange(M), 3)
+        want, size = op.matmul(a[rest], sa[rest], fa, b, sb, 0)
+        assert (np.abs(got[rest] - want) <= (K + 1) * 2.0 ** -23 * size).all()
+
+
+@pytest.mark.parametrize("M,N", [(5, 7), (130, 260), (0, 4), (4, 0)])
+def test_nothing_to_add_up(M, N):
+    q = [torch.empty(r, 0, dtype=torch.float8_e4m3fn, device=DEV) for r in (M, N)]
+    s = [torch.empty(r, 0, dtype=torch.uint8, device=DEV) for r in (M, N)]
+    out, c_in = torch.full((M, N), float("nan"), device=DEV), torch.randn(M, N, device=DEV)
+    ts.ts_matmul_fp8(q[0], s[0], q[1], s[1], 0, out)
+    assert (out == 0).all()
+    ts.ts_matmul_fp8(q[0], s[0], q[1], s[1], 0, out, c_in)
+    assert torch.equal(out, c_in)
+
+
+def test_a_split_product_needs_its_workspace_and_ends_the_views():
+    M, N, K = 64, 128, 1 << 17
+    size = ts.ts_matmul_workspace_bytes(M, N, K)
+    if size == 0:
+        pytest.skip("not split")
+    a, b = ts.fp8_empty(M, K), ts.fp8_empty(N, K)
+    for q, s in (a, b):
+        q.view(torch.uint8).zero_()
+        s.zero_()
+    out = torch.empty(M, N, device=DEV)
+    ts.ts_bind_workspace(None)
+    with pytest.raises(ts.TsError, match="workspace"):
+        ts.ts_matmul_fp8(*a, *b, K, out)
+    n, d, V = 100, 16, 50
+    ws = torch.empty(max(size, ts.ts_workspace_bytes(n, d, V)), dtype=torch.uint8, device=DEV)
+    ts.ts_bind_workspace(ws)
+    try:
+        ids, rows = torch.zeros(n, dtype=torch.int32, device=DEV), torch.zeros(n, d, device=DEV)
+        ts.ts_densify(ids, rows, d, V, None, torch.empty(V, d, device=DEV))
+        ts.ts_last_views()
+        ts.ts_matmul_fp8(*a, *b, K, out)
+        with pytest.raises(ts.TsError):
+            ts.ts_last_views()
+        assert (out == 0).all()
+    finally:
+        ts.ts_bind_workspace(None)
+
+
+def test_in_a_captured_graph():
+    M, N, K = 96, 200, 6000
+    x, w = torch.randn(M, K, device=DEV), torch.randn(N, K, device=DEV)
+    qx, qw = ts.fp8_empty(M, K, E5M2), ts.fp8_empty(N, K)
+    out, c_in = torch.empty(M, N, device=DEV), torch.randn(M, N, device=DEV)
+    ws = bind(M, N, K)
+    try:
+        def work():
+            ts.ts_quantize_fp8(x, E5M2, *qx)
+            ts.ts_matmul_fp8(*qx, *qw, K, out, c_in)
+
+        ts.ts_quantize_fp8(w, E4M3, *qw)
+        s = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            work()
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            work()
+        for k in range(3):
+            x.copy_(torch.randn(M, K, generator=torch.Generator().manual_seed(k)))
+            graph.replay()
+            torch.cuda.synchronize()
+            got = out.clone()
+            work()
+            torch.cuda.synchronize()
+            assert torch.equal(got, out)
+    finally:
+        ts.ts_bind_workspace(None)
+
+
+def test_shapes_and_types_of_the_binding():
+    M, N, K = 4, 8, 200
+    x = torch.randn(M, K, device=DEV)
+    (q, s), (qt, st), (w, sw) = ts.fp8_empty(M, K), ts.fp8_empty(K, M), ts.fp8_empty(N, K)
+    out = torch.empty(M, N, device=DEV)
+    for call in (lambda: ts.ts_quantize_fp8(x, E4M3, q[:, :K], s), lambda: ts.ts_quantize_fp8(x, E5M2, q, s),
+                 lambda: ts.ts_quantize_fp8(x, E4M3, q, s[:, :2]), lambda: ts.ts_quantize_fp8(x, E4M3, qt, st),
+                 lambda: ts.ts_quantize_fp8(x, E4M3, q), lambda: ts.ts_quantize_fp8(x.t(), E4M3, q, s),
+                 lambda: ts.ts_quantize_fp8(x.half(), E4M3, q, s),
+                 lambda: ts.ts_matmul_fp8(q, s, w, sw, K + 128, out), lambda: ts.ts_matmul_fp8(q, s, w, sw, K, out.t()),
+                 lambda: ts.ts_matmul_fp8(q.view(torch.uint8), s, w, sw, K, out), lambda: ts.ts_matmul_fp8(q, s, w, sw, K, out.half()),
+                 lambda: ts.ts_matmul_fp8(q, s, w, sw, K, out, out[:2]), lambda: ts.ts_matmul_fp8(q, s[:, :2], w, sw, K, out),
+                 lambda: ts.ts_matmul_fp8(q, s, w, sw, -1, out)):
+        with pytest.raises(AssertionError):
+            call()
+    with pytest.raises(ts.TsError):
+        ts.ts_quantize_fp8(x, 2, q.view(torch.uint8), s)
+    with pytest.raises(ts.TsError):
+        ts.ts_quantize_fp8(x, E4M3)
+    with pytest.raises(ts.TsError):
+        ts.ts_matmul_fp8(q, s, w, sw, K, out.bfloat16(), torch.zeros(M, N, device=DEV))
