@@ -198,6 +198,10 @@ __global__ __launch_bounds__(256) void quantize_kernel(Quantize p)
 }
 
 // ------------------------------------------------------------------ product
+#define LOAD16(base, off, to) \
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)((base) + (off)), \
+                                     (__attribute__((address_space(3))) void*)(lds + (to)), 16, 0, 0)
+
 struct Matmul {
     const uint8_t *a, *a_scales, *b, *b_scales;
     const float* c_in;
@@ -293,6 +297,129 @@ __global__ __launch_bounds__(256) void matmul_kernel(Matmul p)
     store4<BF16>(p, m, n0 + (lane >> 4) * 4, acc);
 }
 
+// ---- large products: tiles through LDS
+__device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <int FA, int FB, bool BF16, int WN, int WM, int NF, int MF>
+__global__ __launch_bounds__(64 * WN * WM) void tile_kernel(Matmul p)
+{
+    constexpr int TN = 16 * WN * NF, TM = 16 * WM * MF, ROWS = TN + TM, WAVES = WN * WM;
+    constexpr int LOADS = ROWS / (8 * WAVES);                 // of 1 KiB by a wavefront, for one block
+    extern __shared__ __align__(1024) uint8_t lds[];          // [2][ROWS][128]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wn = wave % WN, wm = wave / WN;
+    const int64_t tile = p.tile_first + blockIdx.x;
+    const int64_t m0 = tile / p.n_tiles * TM, n0 = tile % p.n_tiles * TN;
+
+    const auto key = [](int row, bool of_b) { return BF16 && of_b ? (row & 3) | ((row >> 1) & 4) : row & 7; };
+    // where this lane's 16 bytes of each load come from
+    uint32_t from[LOADS];
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+        const int row = (wave * LOADS + j) * 8 + (lane >> 3);
+        const bool of_b = (wave * LOADS + j) * 8 < TN;
+        const int r = of_b ? row : row - TN;
+        const int64_t last = of_b ? p.N - 1 - n0 : p.M - 1 - m0;
+        const int64_t at = r < last ? r : last;
+        from[j] = (uint32_t)(at * p.ld) + (uint32_t)(((lane & 7) ^ key(r, of_b)) * 16);
+    }
+    const uint8_t *const a = p.a + m0 * p.ld, *const b = p.b + n0 * p.ld;
+    const auto fetch = [&](int k, int stage) {
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const bool of_b = (wave * LOADS + j) * 8 < TN;
+            const uint8_t* const base = (of_b ? b : a) + (int64_t)k * kBlock;
+            const uint32_t to = (uint32_t)(stage * ROWS * kBlock + (wave * LOADS + j) * 1024);
+            LOAD16(base, from[j], to);
+        }
+    };
+    // scales: four blocks to a word
+    const uint32_t *sb_at[NF], *sa_at[MF];
+    uint32_t sb[NF], sa[MF], sb_next[NF], sa_next[MF];
+    const int i = lane & 15, g = lane >> 4;
+    const auto n_of = [&](int f) { return BF16 ? (f >> 1) * 32 + (i >> 2) * 8 + (f & 1) * 4 + (i & 3) : f * 16 + i; };
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+        const int64_t n = n0 + wn * NF * 16 + n_of(f);
+        sb_at[f] = (const uint32_t*)(p.b_scales + (n < p.N ? n : p.N - 1) * p.lds);
+        sb_next[f] = *sb_at[f];
+    }
+#pragma unroll
+    for (int f = 0; f < MF; ++f) {
+        const int64_t m = m0 + (wm * MF + f) * 16 + i;
+        sa_at[f] = (const uint32_t*)(p.a_scales + (m < p.M ? m : p.M - 1) * p.lds);
+        sa_next[f] = *sa_at[f];
+    }
+    const uint8_t* const read_b = lds + (wn * NF * 16 + n_of(0)) * kBlock + ((g ^ (i & 7)) << 4);
+    const uint8_t* const read_a = lds + (TN + wm * MF * 16 + i) * kBlock + ((g ^ (i & 7)) << 4);
+    const uint8_t* const read_b4 = lds + (wn * NF * 16 + n_of(0)) * kBlock + (((g ^ (i & 7)) ^ 4) << 4);
+    const uint8_t* const read_a4 = lds + (TN + wm * MF * 16 + i) * kBlock + (((g ^ (i & 7)) ^ 4) << 4);
+    const auto codes = [&](const uint8_t* lo, const uint8_t* hi, int at) {
+        const i4 x = *reinterpret_cast<const i4*>(lo + at), y = *reinterpret_cast<const i4*>(hi + at);
+        return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    f4 acc[NF][MF];
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int h = 0; h < MF; ++h) acc[f][h] = (f4)(0.0f);
+
+    fetch(0, 0);
+    for (int k = 0; k < p.blocks; ++k) {
+        wait_and_meet();
+        if ((k & 3) == 0) {
+#pragma unroll
+            for (int f = 0; f < NF; ++f) sb[f] = sb_next[f];
+#pragma unroll
+            for (int f = 0; f < MF; ++f) sa[f] = sa_next[f];
+        }
+        if (k + 1 < p.blocks) {
+            fetch(k + 1, (k + 1) & 1);
+            if ((k & 3) == 3) {
+#pragma unroll
+                for (int f = 0; f < NF; ++f) sb_next[f] = sb_at[f][(k + 1) >> 2];
+#pragma unroll
+                for (int f = 0; f < MF; ++f) sa_next[f] = sa_at[f][(k + 1) >> 2];
+            }
+        }
+        const int stage = (k & 1) * ROWS * kBlock, shift = (k & 3) * 8;
+        if constexpr (BF16) {
+            i8 v[MF];
+#pragma unroll
+            for (int h = 0; h < MF; ++h) v[h] = codes(read_a, read_a4, stage + h * 16 * kBlock);
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                const i8 u = codes(read_b, read_b4, stage + (f >> 1) * 32 * kBlock + (f & 1) * 4 * kBlock);
+#pragma unroll
+                for (int h = 0; h < MF; ++h)
+                    acc[f][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v[h], acc[f][h], FB, FA, 0, (int)(sb[f] >> shift), 0, (int)(sa[h] >> shift));
+            }
+        } else {
+            b8 v[MF][4];
+#pragma unroll
+            for (int h = 0; h < MF; ++h) widen<FA>(codes(read_a, read_a4, stage + h * 16 * kBlock), (sa[h] >> shift) & 255u, v[h]);
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                b8 u[4];
+                widen<FB>(codes(read_b, read_b4, stage + f * 16 * kBlock), (sb[f] >> shift) & 255u, u);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int h = 0; h < MF; ++h) acc[f][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u[q], v[h][q], acc[f][h], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < MF; ++h) {
+        const int64_t m = m0 + (wm * MF + h) * 16 + i;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            const int64_t n = n0 + wn * NF * 16 + (BF16 ? (f >> 1) * 32 + g * 8 + (f & 1) * 4 : f * 16 + g * 4);
+            store4<BF16>(p, m, n, acc[f][h]);
+        }
+    }
+}
+
 constexpr int64_t kMaxWgs = 1 << 22;      // work-groups per launch (a launch has less than 2^32 threads)
 
 template <typename F>
@@ -311,9 +438,27 @@ void launch_quantize(Quantize p, int64_t tiles, hipStream_t stream)
     });
 }
 
+template <int FA, int FB, bool BF16, int WN, int WM, int NF, int MF>
+void launch_tiles(Matmul p, hipStream_t stream)
+{
+    constexpr int TN = 16 * WN * NF, TM = 16 * WM * MF;
+    p.n_tiles = (p.N + TN - 1) / TN;
+    const int lds = 2 * (TN + TM) * kBlock;
+    const auto kernel = tile_kernel<FA, FB, BF16, WN, WM, NF, MF>;
+    in_launches((p.M + TM - 1) / TM * p.n_tiles, [&](int64_t at, unsigned n) {
+        p.tile_first = at;
+        hipLaunchKernelGGL(kernel, dim3(n), dim3(64 * WN * WM), lds, stream, p);
+    });
+}
+
 template <int FA, int FB>
 void launch_matmul(Matmul p, bool bf16, hipStream_t stream)
 {
+    if (p.blocks > 0 && p.M > 64 && p.N > 64) {          // (a tile's first block is fetched without a question)
+        if (bf16) launch_tiles<FA, FB, true, 2, 4, 8, 4>(p, stream);
+        else launch_tiles<FA, FB, false, 2, 2, 4, 4>(p, stream);
+        return;
+    }
     p.n_tiles = (p.N + 63) / 64;
     in_launches((p.M + 15) / 16 * p.n_tiles, [&](int64_t at, unsigned n) {
         p.tile_first = at;
