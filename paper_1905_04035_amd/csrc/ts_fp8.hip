@@ -14,6 +14,7 @@
 // matrix instructions (16 x 32 by 32 x 16, half the rate), whose products are exact and whose sums are fp32.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <stdlib.h>
 
 #include "ts_densify.h"
 #include "ts_workspace.h"
@@ -198,10 +199,6 @@ __global__ __launch_bounds__(256) void quantize_kernel(Quantize p)
 }
 
 // ------------------------------------------------------------------ product
-#define LOAD16(base, off, to) \
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)((base) + (off)), \
-                                     (__attribute__((address_space(3))) void*)(lds + (to)), 16, 0, 0)
-
 struct Matmul {
     const uint8_t *a, *a_scales, *b, *b_scales;
     const float* c_in;
@@ -210,7 +207,7 @@ struct Matmul {
     int64_t ld, lds;            // bytes of a row of codes and of scales
     int32_t blocks;             // of 128 along K
     int64_t tile_first;
-    int64_t n_tiles;
+    int64_t m_tiles, n_tiles;
 };
 
 // Stores out[m][n .. n + 3].
@@ -264,6 +261,49 @@ __device__ __forceinline__ void widen(i8 codes, uint32_t scale, b8 (&out)[4])
     }
 }
 
+// 16 bytes of a row of the result, at an address that is aligned to an element.
+template <bool BF16>
+struct Out;
+template <>
+struct Out<true> {
+    typedef u4 Vec;
+    static constexpr int BYTES = 2;
+};
+template <>
+struct Out<false> {
+    typedef f4 Vec;
+    static constexpr int BYTES = 4;
+};
+
+template <bool BF16>
+__device__ __forceinline__ void store_row(const Matmul& p, int64_t m, int64_t n, typename Out<BF16>::Vec v)
+{
+    if (n >= p.N) return;
+    const int64_t at = m * p.N + n;
+    if constexpr (BF16) {
+        typedef u4 __attribute__((aligned(2))) any_u4;
+        uint16_t* const out = (uint16_t*)p.out + at;
+        if (n + 8 <= p.N) {
+            __builtin_nontemporal_store(v, reinterpret_cast<any_u4*>(out));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 7; ++j)
+                if (n + j < p.N) out[j] = (uint16_t)(v[j >> 1] >> (j & 1) * 16);
+        }
+    } else {
+        typedef f4 __attribute__((aligned(4))) any_f4;
+        float* const out = (float*)p.out + at;
+        if (n + 4 <= p.N) {
+            if (p.c_in) v += *reinterpret_cast<const any_f4*>(p.c_in + at);
+            __builtin_nontemporal_store(v, reinterpret_cast<any_f4*>(out));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (n + j < p.N) out[j] = p.c_in ? v[j] + p.c_in[at + j] : v[j];
+        }
+    }
+}
+
 __device__ __forceinline__ i8 load_codes(const uint8_t* p)
 {
     const i4 lo = *reinterpret_cast<const i4*>(p), hi = *reinterpret_cast<const i4*>(p + 16);
@@ -298,126 +338,230 @@ __global__ __launch_bounds__(256) void matmul_kernel(Matmul p)
 }
 
 // ---- large products: tiles through LDS
-__device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+typedef __attribute__((address_space(3))) void* lds_ptr;
 
-template <int FA, int FB, bool BF16, int WN, int WM, int NF, int MF>
-__global__ __launch_bounds__(64 * WN * WM) void tile_kernel(Matmul p)
+// Waits for this wavefront's loads into LDS and its reads from it, then for the work-group's other wavefronts.
+// (all but the LATER last ones)
+template <int LATER = 0>
+__device__ __forceinline__ void wait_and_meet()
 {
-    constexpr int TN = 16 * WN * NF, TM = 16 * WM * MF, ROWS = TN + TM, WAVES = WN * WM;
-    constexpr int LOADS = ROWS / (8 * WAVES);                 // of 1 KiB by a wavefront, for one block
-    extern __shared__ __align__(1024) uint8_t lds[];          // [2][ROWS][128]
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wn = wave % WN, wm = wave / WN;
-    const int64_t tile = p.tile_first + blockIdx.x;
-    const int64_t m0 = tile / p.n_tiles * TM, n0 = tile % p.n_tiles * TN;
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER < 63 ? LATER : 63) : "memory");
+}
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0); }
 
-    const auto key = [](int row, bool of_b) { return BF16 && of_b ? (row & 3) | ((row >> 1) & 4) : row & 7; };
-    // where this lane's 16 bytes of each load come from
-    uint32_t from[LOADS];
+#ifdef __HIP_DEVICE_COMPILE__
+// A part of an operand as a buffer: reads beyond `bytes` give zeros.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const uint8_t* p, int64_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, (int)(uint32_t)(bytes < 0xFFFFFFFFll ? bytes : 0xFFFFFFFFll), 0x00020000);
+}
+#endif
+
+// The t-th tile.  Work-groups b, b + 8, b + 16, ... run on one of eight XCDs with an L2 each: every XCD takes neighbouring tiles, kStrip of them along
+// M before the next along N, so that those it works on at one time share their operands, and write long stretches of the result's rows.
+// 8192 x 32768 x 1024 to bf16 with strips of 1 / 2 / 4 / 8 / 16: 310 / 299 / 290 / 325 / 327 us, 8192^3 487 / 459 / 460 / 469 / 470.
+constexpr int kStrip = 4;
+
+__device__ __forceinline__ void place(int64_t wg, int64_t m_tiles, int64_t n_tiles, int64_t* mt, int64_t* nt)
+{
+    const int64_t tiles = m_tiles * n_tiles, each = tiles >> 3, rest = tiles & 7, x = wg & 7;
+    const int64_t t = x * each + (x < rest ? x : rest) + (wg >> 3);
+    const int64_t strip = kStrip * n_tiles, s = t / strip, at = t - s * strip;
+    const int64_t high = m_tiles - s * kStrip < kStrip ? m_tiles - s * kStrip : kStrip;
+    *nt = at / high;
+    *mt = s * kStrip + (at - *nt * high);
+}
+
+template <int FA, int FB, bool BF16, int WN, int WM, int NF, int MF, int PER_SIMD>
+__global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
+{
+#ifdef __HIP_DEVICE_COMPILE__     // (a buffer's type is none of the host compiler's)
+    constexpr int TN = 16 * WN * NF, TM = 16 * WM * MF, ROWS = TN + TM, WAVES = WN * WM;
+    constexpr int LB = TN / (8 * WAVES), LA = TM / (8 * WAVES);     // loads of 1 KiB by a wavefront, for one block
+    constexpr int STAGE = ROWS * kBlock, SCALES = 2 * STAGE;
+    static_assert(TN % (8 * WAVES) == 0 && TM % (8 * WAVES) == 0 && TN % 64 == 0 && TM % 64 == 0, "whole loads");
+    extern __shared__ __align__(1024) uint8_t lds[];          // two stages of [ROWS][128] codes, two of [ROWS] words of scales
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wn = wave % WN, wm = wave / WN, i = lane & 15, g = lane >> 4;
+    // Row r of a stage: of B for r < TN, else of A; its 16-byte chunk c lies in slot c ^ key(r), so that sixteen lanes that read
+    // one chunk of sixteen rows meet no bank twice.  With a bf16 result, rows of two fragments of B are interleaved by fours (n_of), and the
+    // four columns that a lane has of each lie side by side.
+    const auto n_of = [&](int f) { return BF16 ? (f >> 1) * 32 + (i >> 2) * 8 + (f & 1) * 4 + (i & 3) : f * 16 + i; };
+    const uint32_t ld = (uint32_t)p.ld, rb = (uint32_t)(wave * LB * 8 + (lane >> 3)), ra = (uint32_t)(wave * LA * 8 + (lane >> 3));
+    const uint32_t key_b = BF16 ? (rb & 3) | ((rb >> 1) & 4) : rb & 7;
+    const uint32_t from_b = rb * ld + (((lane & 7) ^ key_b) << 4), from_a = ra * ld + (((lane & 7) ^ (ra & 7)) << 4);
+    uint32_t row_b[LB], row_a[LA];
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) {
-        const int row = (wave * LOADS + j) * 8 + (lane >> 3);
-        const bool of_b = (wave * LOADS + j) * 8 < TN;
-        const int r = of_b ? row : row - TN;
-        const int64_t last = of_b ? p.N - 1 - n0 : p.M - 1 - m0;
-        const int64_t at = r < last ? r : last;
-        from[j] = (uint32_t)(at * p.ld) + (uint32_t)(((lane & 7) ^ key(r, of_b)) * 16);
-    }
-    const uint8_t *const a = p.a + m0 * p.ld, *const b = p.b + n0 * p.ld;
-    const auto fetch = [&](int k, int stage) {
+    for (int j = 0; j < LB; ++j) row_b[j] = (BF16 && (j & 1) ? from_b ^ 64 : from_b) + j * 8 * ld;    // (eight rows on, the key's third bit is the other one)
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            const bool of_b = (wave * LOADS + j) * 8 < TN;
-            const uint8_t* const base = (of_b ? b : a) + (int64_t)k * kBlock;
-            const uint32_t to = (uint32_t)(stage * ROWS * kBlock + (wave * LOADS + j) * 1024);
-            LOAD16(base, from[j], to);
+    for (int j = 0; j < LA; ++j) row_a[j] = from_a + j * 8 * ld;
+    // the tile that is fetched
+    int64_t m0, n0, m_here, n_here;
+    const uint8_t *a, *b, *sa_from, *sb_from;
+    const auto turn_to = [&](int64_t t) {
+        int64_t mt, nt;
+        place(t, p.m_tiles, p.n_tiles, &mt, &nt);
+        m0 = mt * TM;
+        n0 = nt * TN;
+        m_here = p.M - m0 < TM ? p.M - m0 : TM;
+        n_here = p.N - n0 < TN ? p.N - n0 : TN;
+        a = p.a + m0 * p.ld;
+        b = p.b + n0 * p.ld;
+        sa_from = p.a_scales + m0 * p.lds;
+        sb_from = p.b_scales + n0 * p.lds;
+    };
+    // Load j of this wavefront's share of block k (codes of B, of A, words of four scales), into stage k % 2.  Behind the last block: zeros, without
+    // a question, so that the loop below stays one run of instructions that keeps its order.
+    constexpr int LS = (ROWS / 64 + WAVES - 1) / WAVES, LOADS = LB + LA + LS;
+    const auto fetch = [&](int k, int j) {
+        const bool there = k < p.blocks;
+        uint8_t* const to = lds + (k & 1) * STAGE;
+        const int at_k = there ? k * kBlock : 0;            // (never more than a buffer's length)
+        if (j < LB) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(b, there ? n_here * p.ld : 0), (lds_ptr)(to + (wave * LB + j) * 1024), 16, row_b[j], at_k, 0, 0);
+        } else if (j < LB + LA) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(a, there ? m_here * p.ld : 0), (lds_ptr)(to + TN * kBlock + (wave * LA + j - LB) * 1024), 16,
+                                                     row_a[j - LB], at_k, 0, 0);
+        } else {
+            const int k4 = (there ? k : p.blocks - 1) >> 2;
+            const int at = (wave + (j - LB - LA) * WAVES) % (ROWS / 64);        // (more wavefronts than words: some are fetched twice)
+            const bool of_b = at * 64 < TN;
+            const __amdgpu_buffer_rsrc_t words = buffer(of_b ? sb_from : sa_from, (of_b ? n_here : m_here) * p.lds);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(words, (lds_ptr)(lds + SCALES + (k4 & 1) * ROWS * 4 + at * 256), 4,
+                                                     (uint32_t)(at * 64 + lane - (of_b ? 0 : TN)) * (uint32_t)p.lds, k4 * 4, 0, 0);
         }
     };
-    // scales: four blocks to a word
-    const uint32_t *sb_at[NF], *sa_at[MF];
-    uint32_t sb[NF], sa[MF], sb_next[NF], sa_next[MF];
-    const int i = lane & 15, g = lane >> 4;
-    const auto n_of = [&](int f) { return BF16 ? (f >> 1) * 32 + (i >> 2) * 8 + (f & 1) * 4 + (i & 3) : f * 16 + i; };
-#pragma unroll
-    for (int f = 0; f < NF; ++f) {
-        const int64_t n = n0 + wn * NF * 16 + n_of(f);
-        sb_at[f] = (const uint32_t*)(p.b_scales + (n < p.N ? n : p.N - 1) * p.lds);
-        sb_next[f] = *sb_at[f];
-    }
-#pragma unroll
-    for (int f = 0; f < MF; ++f) {
-        const int64_t m = m0 + (wm * MF + f) * 16 + i;
-        sa_at[f] = (const uint32_t*)(p.a_scales + (m < p.M ? m : p.M - 1) * p.lds);
-        sa_next[f] = *sa_at[f];
-    }
-    const uint8_t* const read_b = lds + (wn * NF * 16 + n_of(0)) * kBlock + ((g ^ (i & 7)) << 4);
-    const uint8_t* const read_a = lds + (TN + wm * MF * 16 + i) * kBlock + ((g ^ (i & 7)) << 4);
-    const uint8_t* const read_b4 = lds + (wn * NF * 16 + n_of(0)) * kBlock + (((g ^ (i & 7)) ^ 4) << 4);
-    const uint8_t* const read_a4 = lds + (TN + wm * MF * 16 + i) * kBlock + (((g ^ (i & 7)) ^ 4) << 4);
-    const auto codes = [&](const uint8_t* lo, const uint8_t* hi, int at) {
-        const i4 x = *reinterpret_cast<const i4*>(lo + at), y = *reinterpret_cast<const i4*>(hi + at);
+    // places of this lane's codes in a stage, chunk g and chunk g + 4 of a row
+    const int at_b = (wn * NF * 16 + n_of(0)) * kBlock, at_a = (TN + wm * MF * 16 + i) * kBlock, lo = (g ^ (i & 7)) << 4, hi = lo ^ 64;
+    const auto codes = [&](int at) {
+        const i4 x = *reinterpret_cast<const i4*>(lds + at + lo), y = *reinterpret_cast<const i4*>(lds + at + hi);
         return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    f4 acc[NF][MF];
+    const auto codes_b = [&](int stage, int f) { return codes(stage + at_b + (BF16 ? (f >> 1) * 32 + (f & 1) * 4 : f * 16) * kBlock); };
+    const auto codes_a = [&](int stage, int h) { return codes(stage + at_a + h * 16 * kBlock); };
+    uint32_t sb[NF], sa[MF];
+    const auto scales = [&](int k) {
+        const uint8_t* const at = lds + SCALES + (k >> 2 & 1) * ROWS * 4;
 #pragma unroll
-    for (int f = 0; f < NF; ++f)
+        for (int f = 0; f < NF; ++f) sb[f] = *reinterpret_cast<const uint32_t*>(at + (wn * NF * 16 + n_of(f)) * 4);
 #pragma unroll
-        for (int h = 0; h < MF; ++h) acc[f][h] = (f4)(0.0f);
-
-    fetch(0, 0);
-    for (int k = 0; k < p.blocks; ++k) {
+        for (int h = 0; h < MF; ++h) sa[h] = *reinterpret_cast<const uint32_t*>(at + (TN + (wm * MF + h) * 16 + i) * 4);
+    };
+    // A block's last fragment of B is multiplied behind the meeting that ends its stage, while the next block's first codes are
+    // on their way from LDS; the loads of the block after that, into the stage that the meeting has set free, are spread over the first
+    // half of the next block, so that none of them holds up a read from LDS that a multiplication waits for.
+    constexpr int SPREAD = NF > 4 ? NF / 2 : NF - 1, AT_ONCE = (LOADS + SPREAD - 1) / SPREAD;
+    typedef typename Out<BF16>::Vec Vec;
+    constexpr int PER_VEC = 16 / Out<BF16>::BYTES, EF = BF16 ? NF : NF / 2, VECS = EF * 16 / PER_VEC, PITCH = EF * 16 * Out<BF16>::BYTES + 16, TURN = 64 / VECS;
+    static_assert(WAVES * 16 * PITCH <= STAGE && 64 % VECS == 0 && 16 % TURN == 0, "room for every wavefront; whole rows");
+    constexpr int STORES = MF * (NF / EF) * (16 / TURN);
+    const int64_t tiles = p.m_tiles * p.n_tiles;
+    int64_t tile = blockIdx.x;
+    turn_to(tile);
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) fetch(0, j);
+    wait_and_meet();
+    for (;;) {
+        f4 acc[NF][MF];
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int h = 0; h < MF; ++h) acc[f][h] = (f4)(0.0f);
+        scales(0);
+        i8 u = codes_b(0, 0), v[MF];
+        b8 wide[MF][4];
+#pragma unroll
+        for (int h = 0; h < MF; ++h) v[h] = codes_a(0, h);
+        if constexpr (!BF16) {
+#pragma unroll
+            for (int h = 0; h < MF; ++h) widen<FA>(v[h], sa[h] & 255u, wide[h]);
+        }
+        for (int k = 0; k < p.blocks; ++k) {
+            const int stage = (k & 1) * STAGE, next = STAGE - stage;
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                if (f + 1 == NF) wait_and_meet();
+                const i8 un = f + 1 < NF ? codes_b(stage, f + 1) : codes_b(next, 0);
+                keep_order();
+#pragma unroll
+                for (int j = f * AT_ONCE; j < (f + 1) * AT_ONCE; ++j)
+                    if (j < LOADS) fetch(k + 1, j);
+                b8 x[4];
+                if constexpr (!BF16) widen<FB>(u, sb[f] & 255u, x);
+#pragma unroll
+                for (int h = 0; h < MF; ++h) {
+                    if constexpr (BF16) {
+                        acc[f][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v[h], acc[f][h], FB, FA, 0, (int)sb[f], 0, (int)sa[h]);
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) acc[f][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[q], wide[h][q], acc[f][h], 0, 0, 0);
+                    }
+                    if (f + 1 == NF) {
+                        keep_order();
+                        v[h] = codes_a(next, h);
+                        keep_order();
+                    }
+                }
+                keep_order();
+                u = un;
+            }
+            scales(k + 1);
+            const int shift = ((k + 1) & 3) * 8;
+#pragma unroll
+            for (int f = 0; f < NF; ++f) sb[f] >>= shift;
+#pragma unroll
+            for (int h = 0; h < MF; ++h) sa[h] >>= shift;
+            if constexpr (!BF16) {
+#pragma unroll
+                for (int h = 0; h < MF; ++h) widen<FA>(v[h], sa[h] & 255u, wide[h]);
+            }
+        }
+        // The next tile's first block is on its way, into stage 0, while this tile's result leaves through stage 1: sixteen rows at a time, so that a
+        // wavefront stores whole stretches of 256 bytes; each has a place of its own, and waits for nobody.
         wait_and_meet();
-        if ((k & 3) == 0) {
+        const int64_t m_out = m0 + wm * MF * 16 + lane / VECS, n_out = n0 + wn * NF * 16 + (lane % VECS) * PER_VEC;
+        const bool whole = m_here == TM && n_here == TN;
+        tile += gridDim.x;
+        if (tile < tiles) {
+            turn_to(tile);
 #pragma unroll
-            for (int f = 0; f < NF; ++f) sb[f] = sb_next[f];
-#pragma unroll
-            for (int f = 0; f < MF; ++f) sa[f] = sa_next[f];
+            for (int j = 0; j < LOADS; ++j) fetch(0, j);
         }
-        if (k + 1 < p.blocks) {
-            fetch(k + 1, (k + 1) & 1);
-            if ((k & 3) == 3) {
+        uint8_t* const mine = lds + STAGE + wave * 16 * PITCH;
 #pragma unroll
-                for (int f = 0; f < NF; ++f) sb_next[f] = sb_at[f][(k + 1) >> 2];
+        for (int h = 0; h < MF; ++h) {
 #pragma unroll
-                for (int f = 0; f < MF; ++f) sa_next[f] = sa_at[f][(k + 1) >> 2];
+            for (int e = 0; e < NF; e += EF) {
+#pragma unroll
+                for (int f = e; f < e + EF; ++f) {
+                    if constexpr (BF16) {
+                        if (f & 1) {
+                            const u4 w = {narrow2(acc[f - 1][h].x, acc[f - 1][h].y), narrow2(acc[f - 1][h].z, acc[f - 1][h].w),
+                                          narrow2(acc[f][h].x, acc[f][h].y), narrow2(acc[f][h].z, acc[f][h].w)};
+                            *reinterpret_cast<u4*>(mine + i * PITCH + ((f >> 1) * 32 + g * 8) * 2) = w;
+                        }
+                    } else {
+                        *reinterpret_cast<f4*>(mine + i * PITCH + ((f - e) * 16 + g * 4) * 4) = acc[f][h];
+                    }
+                }
+                __builtin_amdgcn_wave_barrier();
+                Vec out[16 / TURN];
+#pragma unroll
+                for (int t = 0; t < 16 / TURN; ++t) out[t] = *reinterpret_cast<const Vec*>(mine + (t * TURN + lane / VECS) * PITCH + (lane % VECS) * 16);
+#pragma unroll
+                for (int t = 0; t < 16 / TURN; ++t) {
+                    const int64_t m = m_out + h * 16 + t * TURN;
+                    if (m < p.M) store_row<BF16>(p, m, n_out + e * 16, out[t]);
+                }
+                __builtin_amdgcn_wave_barrier();
             }
         }
-        const int stage = (k & 1) * ROWS * kBlock, shift = (k & 3) * 8;
-        if constexpr (BF16) {
-            i8 v[MF];
-#pragma unroll
-            for (int h = 0; h < MF; ++h) v[h] = codes(read_a, read_a4, stage + h * 16 * kBlock);
-#pragma unroll
-            for (int f = 0; f < NF; ++f) {
-                const i8 u = codes(read_b, read_b4, stage + (f >> 1) * 32 * kBlock + (f & 1) * 4 * kBlock);
-#pragma unroll
-                for (int h = 0; h < MF; ++h)
-                    acc[f][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v[h], acc[f][h], FB, FA, 0, (int)(sb[f] >> shift), 0, (int)(sa[h] >> shift));
-            }
-        } else {
-            b8 v[MF][4];
-#pragma unroll
-            for (int h = 0; h < MF; ++h) widen<FA>(codes(read_a, read_a4, stage + h * 16 * kBlock), (sa[h] >> shift) & 255u, v[h]);
-#pragma unroll
-            for (int f = 0; f < NF; ++f) {
-                b8 u[4];
-                widen<FB>(codes(read_b, read_b4, stage + f * 16 * kBlock), (sb[f] >> shift) & 255u, u);
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int h = 0; h < MF; ++h) acc[f][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u[q], v[h][q], acc[f][h], 0, 0, 0);
-            }
-        }
+        if (tile >= tiles) return;
+        // the loads are older than the stores: where every store was made, these may still be on their way
+        if (whole && !p.c_in) wait_and_meet<STORES>();
+        else wait_and_meet();
     }
-#pragma unroll
-    for (int h = 0; h < MF; ++h) {
-        const int64_t m = m0 + (wm * MF + h) * 16 + i;
-#pragma unroll
-        for (int f = 0; f < NF; ++f) {
-            const int64_t n = n0 + wn * NF * 16 + (BF16 ? (f >> 1) * 32 + g * 8 + (f & 1) * 4 : f * 16 + g * 4);
-            store4<BF16>(p, m, n, acc[f][h]);
-        }
-    }
+#endif
 }
 
 constexpr int64_t kMaxWgs = 1 << 22;      // work-groups per launch (a launch has less than 2^32 threads)
@@ -426,6 +570,16 @@ template <typename F>
 void in_launches(int64_t tiles, F&& launch)
 {
     for (int64_t at = 0; at < tiles; at += kMaxWgs) launch(at, (unsigned)(tiles - at < kMaxWgs ? tiles - at : kMaxWgs));
+}
+
+// Compute units of the current GPU.
+int compute_units()
+{
+    static int of[16];
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 16) return 256;
+    if (of[dev] == 0) of[dev] = hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0 ? n : 256;
+    return of[dev];
 }
 
 template <typename T, int FMT>
@@ -438,25 +592,34 @@ void launch_quantize(Quantize p, int64_t tiles, hipStream_t stream)
     });
 }
 
-template <int FA, int FB, bool BF16, int WN, int WM, int NF, int MF>
+template <int FA, int FB, bool BF16, int WN, int WM, int NF, int MF, int PER_SIMD>
 void launch_tiles(Matmul p, hipStream_t stream)
 {
     constexpr int TN = 16 * WN * NF, TM = 16 * WM * MF;
     p.n_tiles = (p.N + TN - 1) / TN;
-    const int lds = 2 * (TN + TM) * kBlock;
-    const auto kernel = tile_kernel<FA, FB, BF16, WN, WM, NF, MF>;
-    in_launches((p.M + TM - 1) / TM * p.n_tiles, [&](int64_t at, unsigned n) {
-        p.tile_first = at;
-        hipLaunchKernelGGL(kernel, dim3(n), dim3(64 * WN * WM), lds, stream, p);
-    });
+    p.m_tiles = (p.M + TM - 1) / TM;
+    const int lds = 2 * (TN + TM) * (kBlock + 4);
+    const auto kernel = tile_kernel<FA, FB, BF16, WN, WM, NF, MF, PER_SIMD>;
+    const int64_t tiles = p.m_tiles * p.n_tiles, most = (int64_t)compute_units() * (160 * 1024 / lds);      // as many work-groups as there is room for
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles < most ? tiles : most)), dim3(64 * WN * WM), lds, stream, p);
 }
 
 template <int FA, int FB>
 void launch_matmul(Matmul p, bool bf16, hipStream_t stream)
 {
     if (p.blocks > 0 && p.M > 64 && p.N > 64) {          // (a tile's first block is fetched without a question)
-        if (bf16) launch_tiles<FA, FB, true, 2, 4, 8, 4>(p, stream);
-        else launch_tiles<FA, FB, false, 2, 2, 4, 4>(p, stream);
+        static const int v = getenv("MMV") ? atoi(getenv("MMV")) : 0;
+        if (bf16) {
+            if (v == 0) launch_tiles<FA, FB, true, 2, 4, 8, 4, 2>(p, stream);
+            else if (v == 1) launch_tiles<FA, FB, true, 2, 2, 8, 8, 1>(p, stream);
+            else if (v == 2) launch_tiles<FA, FB, true, 2, 2, 4, 4, 2>(p, stream);
+            else launch_tiles<FA, FB, true, 4, 2, 4, 8, 2>(p, stream);
+        } else {
+            if (v == 0) launch_tiles<FA, FB, false, 2, 2, 4, 4, 2>(p, stream);
+            else if (v == 1) launch_tiles<FA, FB, false, 2, 4, 8, 4, 2>(p, stream);
+            else if (v == 2) launch_tiles<FA, FB, false, 2, 2, 8, 8, 1>(p, stream);
+            else launch_tiles<FA, FB, false, 4, 2, 4, 4, 2>(p, stream);
+        }
         return;
     }
     p.n_tiles = (p.N + 63) / 64;
