@@ -380,7 +380,7 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
     constexpr int LB = TN / (8 * WAVES), LA = TM / (8 * WAVES);     // loads of 1 KiB by a wavefront, for one block
     constexpr int STAGE = ROWS * kBlock, SCALES = 2 * STAGE;
     static_assert(TN % (8 * WAVES) == 0 && TM % (8 * WAVES) == 0 && TN % 64 == 0 && TM % 64 == 0, "whole loads");
-    extern __shared__ __align__(1024) uint8_t lds[];          // two stages of [ROWS][128] codes, two of [ROWS] words of scales
+    extern __shared__ __align__(1024) uint8_t lds[];          // two stages of [ROWS][128] codes, two of [ROWS] words of scales, 256 bytes that nobody reads
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wn = wave % WN, wm = wave / WN, i = lane & 15, g = lane >> 4;
     // Row r of a stage: of B for r < TN, else of A; its 16-byte chunk c lies in slot c ^ key(r), so that sixteen lanes that read
@@ -423,12 +423,13 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(a, there ? m_here * p.ld : 0), (lds_ptr)(to + TN * kBlock + (wave * LA + j - LB) * 1024), 16,
                                                      row_a[j - LB], at_k, 0, 0);
         } else {
-            const int k4 = (there ? k : p.blocks - 1) >> 2;
+            // every fourth block has new words; else nothing is read, and zeros go where nobody looks
+            const bool words = there && (k & 3) == 0;
             const int at = (wave + (j - LB - LA) * WAVES) % (ROWS / 64);        // (more wavefronts than words: some are fetched twice)
             const bool of_b = at * 64 < TN;
-            const __amdgpu_buffer_rsrc_t words = buffer(of_b ? sb_from : sa_from, (of_b ? n_here : m_here) * p.lds);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(words, (lds_ptr)(lds + SCALES + (k4 & 1) * ROWS * 4 + at * 256), 4,
-                                                     (uint32_t)(at * 64 + lane - (of_b ? 0 : TN)) * (uint32_t)p.lds, k4 * 4, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(of_b ? sb_from : sa_from, words ? (of_b ? n_here : m_here) * p.lds : 0),
+                                                     (lds_ptr)(lds + SCALES + (words ? (k >> 2 & 1) * ROWS * 4 + at * 256 : 2 * ROWS * 4)), 4,
+                                                     (uint32_t)(at * 64 + lane - (of_b ? 0 : TN)) * (uint32_t)p.lds, words ? k : 0, 0, 0);
         }
     };
     // places of this lane's codes in a stage, chunk g and chunk g + 4 of a row
@@ -598,7 +599,7 @@ void launch_tiles(Matmul p, hipStream_t stream)
     constexpr int TN = 16 * WN * NF, TM = 16 * WM * MF;
     p.n_tiles = (p.N + TN - 1) / TN;
     p.m_tiles = (p.M + TM - 1) / TM;
-    const int lds = 2 * (TN + TM) * (kBlock + 4);
+    const int lds = 2 * (TN + TM) * (kBlock + 4) + 256;
     const auto kernel = tile_kernel<FA, FB, BF16, WN, WM, NF, MF, PER_SIMD>;
     const int64_t tiles = p.m_tiles * p.n_tiles, most = (int64_t)compute_units() * (160 * 1024 / lds);      // as many work-groups as there is room for
     hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles < most ? tiles : most)), dim3(64 * WN * WM), lds, stream, p);
