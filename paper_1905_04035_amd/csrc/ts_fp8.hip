@@ -347,6 +347,14 @@ __device__ __forceinline__ void wait_and_meet()
 {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER < 63 ? LATER : 63) : "memory");
 }
+// The same for all of them, or, behind stores that lie after the loads in question, for all but the LATER last.
+template <int LATER>
+__device__ __forceinline__ void meet_behind_stores(bool behind)
+{
+    asm volatile("s_cmp_lg_u32 %1, 0\n\ts_cbranch_scc1 .Lstores_%=\n\ts_waitcnt vmcnt(0)\n.Lstores_%=:\n\ts_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier"
+                 ::"n"(LATER < 63 ? LATER : 63), "s"((int)behind) : "memory", "scc");
+}
+
 __device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0); }
 
 #ifdef __HIP_DEVICE_COMPILE__
@@ -372,15 +380,24 @@ __device__ __forceinline__ void place(int64_t wg, int64_t m_tiles, int64_t n_til
     *mt = s * kStrip + (at - *nt * high);
 }
 
+// Sizes that the host needs, too.  LDS: two stages of [ROWS][128] codes, two of [ROWS] words of scales, 1 KiB that nobody reads, and eight rows of
+// the result for every wavefront.
+template <bool BF16, int WN, int WM, int NF, int MF>
+struct Tile {
+    static constexpr int TN = 16 * WN * NF, TM = 16 * WM * MF, ROWS = TN + TM, STAGE = ROWS * kBlock, SCALES = 2 * STAGE, UNREAD = SCALES + 2 * ROWS * 4;
+    static constexpr int EF = BF16 ? NF : NF / 2, PITCH = EF * 16 * (BF16 ? 2 : 4) + 16;       // fragments of a turn of the result; bytes of a row
+    static constexpr int RESULT = UNREAD + 1024, LDS = RESULT + WN * WM * 8 * PITCH;
+};
+
 template <int FA, int FB, bool BF16, int WN, int WM, int NF, int MF, int PER_SIMD>
 __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
 {
 #ifdef __HIP_DEVICE_COMPILE__     // (a buffer's type is none of the host compiler's)
-    constexpr int TN = 16 * WN * NF, TM = 16 * WM * MF, ROWS = TN + TM, WAVES = WN * WM;
+    typedef Tile<BF16, WN, WM, NF, MF> T;
+    constexpr int TN = T::TN, TM = T::TM, ROWS = T::ROWS, STAGE = T::STAGE, SCALES = T::SCALES, WAVES = WN * WM;
     constexpr int LB = TN / (8 * WAVES), LA = TM / (8 * WAVES);     // loads of 1 KiB by a wavefront, for one block
-    constexpr int STAGE = ROWS * kBlock, SCALES = 2 * STAGE;
     static_assert(TN % (8 * WAVES) == 0 && TM % (8 * WAVES) == 0 && TN % 64 == 0 && TM % 64 == 0, "whole loads");
-    extern __shared__ __align__(1024) uint8_t lds[];          // two stages of [ROWS][128] codes, two of [ROWS] words of scales, 256 bytes that nobody reads
+    extern __shared__ __align__(1024) uint8_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wn = wave % WN, wm = wave / WN, i = lane & 15, g = lane >> 4;
     // Row r of a stage: of B for r < TN, else of A; its 16-byte chunk c lies in slot c ^ key(r), so that sixteen lanes that read
@@ -413,14 +430,15 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
     // Load j of this wavefront's share of block k (codes of B, of A, words of four scales), into stage k % 2.  Behind the last block: zeros, without
     // a question, so that the loop below stays one run of instructions that keeps its order.
     constexpr int LS = (ROWS / 64 + WAVES - 1) / WAVES, LOADS = LB + LA + LS;
-    const auto fetch = [&](int k, int j) {
-        const bool there = k < p.blocks;
-        uint8_t* const to = lds + (k & 1) * STAGE;
+    const auto fetch = [&](int k, int j, bool wanted = true) {
+        const bool there = wanted && k < p.blocks;
+        uint8_t* const to = wanted ? lds + (k & 1) * STAGE : nullptr;          // (a load that was made before: to where nobody looks)
+        uint8_t* const unread = lds + T::UNREAD;
         const int at_k = there ? k * kBlock : 0;            // (never more than a buffer's length)
         if (j < LB) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(b, there ? n_here * p.ld : 0), (lds_ptr)(to + (wave * LB + j) * 1024), 16, row_b[j], at_k, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(b, there ? n_here * p.ld : 0), (lds_ptr)(wanted ? to + (wave * LB + j) * 1024 : unread), 16, row_b[j], at_k, 0, 0);
         } else if (j < LB + LA) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(a, there ? m_here * p.ld : 0), (lds_ptr)(to + TN * kBlock + (wave * LA + j - LB) * 1024), 16,
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(a, there ? m_here * p.ld : 0), (lds_ptr)(wanted ? to + TN * kBlock + (wave * LA + j - LB) * 1024 : unread), 16,
                                                      row_a[j - LB], at_k, 0, 0);
         } else {
             // every fourth block has new words; else nothing is read, and zeros go where nobody looks
@@ -428,7 +446,7 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
             const int at = (wave + (j - LB - LA) * WAVES) % (ROWS / 64);        // (more wavefronts than words: some are fetched twice)
             const bool of_b = at * 64 < TN;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(of_b ? sb_from : sa_from, words ? (of_b ? n_here : m_here) * p.lds : 0),
-                                                     (lds_ptr)(lds + SCALES + (words ? (k >> 2 & 1) * ROWS * 4 + at * 256 : 2 * ROWS * 4)), 4,
+                                                     (lds_ptr)(words ? lds + SCALES + (k >> 2 & 1) * ROWS * 4 + at * 256 : unread), 4,
                                                      (uint32_t)(at * 64 + lane - (of_b ? 0 : TN)) * (uint32_t)p.lds, words ? k : 0, 0, 0);
         }
     };
@@ -451,17 +469,22 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
     // A block's last fragment of B is multiplied behind the meeting that ends its stage, while the next block's first codes are
     // on their way from LDS; the loads of the block after that, into the stage that the meeting has set free, are spread over the first
     // half of the next block, so that none of them holds up a read from LDS that a multiplication waits for.
-    constexpr int SPREAD = NF > 4 ? NF / 2 : NF - 1, AT_ONCE = (LOADS + SPREAD - 1) / SPREAD;
+    constexpr int SPREAD = BF16 ? NF : NF > 4 ? NF / 2 : NF - 1, AT_ONCE = (LOADS + SPREAD - 1) / SPREAD;
     typedef typename Out<BF16>::Vec Vec;
-    constexpr int PER_VEC = 16 / Out<BF16>::BYTES, EF = BF16 ? NF : NF / 2, VECS = EF * 16 / PER_VEC, PITCH = EF * 16 * Out<BF16>::BYTES + 16, TURN = 64 / VECS;
-    static_assert(WAVES * 16 * PITCH <= STAGE && 64 % VECS == 0 && 16 % TURN == 0, "room for every wavefront; whole rows");
+    constexpr int PER_VEC = 16 / Out<BF16>::BYTES, EF = T::EF, VECS = EF * 16 / PER_VEC, PITCH = T::PITCH, TURN = 64 / VECS;
+    static_assert(64 % VECS == 0 && 8 % TURN == 0, "whole rows");
     constexpr int STORES = MF * (NF / EF) * (16 / TURN);
+    // loads of the block after the next that are made before the next one begins
+    constexpr int FIRST = !BF16 ? 0 : NF / 2 * AT_ONCE < LOADS ? NF / 2 * AT_ONCE : LOADS;
     const int64_t tiles = p.m_tiles * p.n_tiles;
     int64_t tile = blockIdx.x;
     turn_to(tile);
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) fetch(0, j);
-    wait_and_meet();
+#pragma unroll
+    for (int j = 0; j < (BF16 ? LOADS : 0); ++j) fetch(1, j);
+    wait_and_meet<BF16 ? LOADS : 0>();
+    bool behind = false;        // stores of the last tile lie between the loads
     for (;;) {
         f4 acc[NF][MF];
 #pragma unroll
@@ -479,32 +502,64 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
         }
         for (int k = 0; k < p.blocks; ++k) {
             const int stage = (k & 1) * STAGE, next = STAGE - stage;
+            if constexpr (BF16) {
+                // First half of the fragments of B: each is multiplied while the one after it is read, and the second half's are read besides.
+                constexpr int H = NF / 2;
+                i8 w[H];
 #pragma unroll
-            for (int f = 0; f < NF; ++f) {
-                if (f + 1 == NF) wait_and_meet();
-                const i8 un = f + 1 < NF ? codes_b(stage, f + 1) : codes_b(next, 0);
-                keep_order();
+                for (int f = 0; f < H; ++f) {
+                    i8 un = u;
+                    if (f + 1 < H) un = codes_b(stage, f + 1);
+                    w[f] = codes_b(stage, H + f);
+                    keep_order();
 #pragma unroll
-                for (int j = f * AT_ONCE; j < (f + 1) * AT_ONCE; ++j)
-                    if (j < LOADS) fetch(k + 1, j);
-                b8 x[4];
-                if constexpr (!BF16) widen<FB>(u, sb[f] & 255u, x);
+                    for (int j = (H + f) * AT_ONCE; j < (H + f + 1) * AT_ONCE; ++j)
+                        if (j < LOADS) fetch(k + 1, j, k > 0);
+#pragma unroll
+                    for (int h = 0; h < MF; ++h)
+                        acc[f][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v[h], acc[f][h], FB, FA, 0, (int)sb[f], 0, (int)sa[h]);
+                    keep_order();
+                    u = un;
+                }
+                // All of this stage is in registers: it is given back.  Second half: as soon as a fragment of A is done with, the next block's is read.
+                meet_behind_stores<STORES + LOADS - FIRST>(behind && k == 0);
+                u = codes_b(next, 0);
 #pragma unroll
                 for (int h = 0; h < MF; ++h) {
-                    if constexpr (BF16) {
-                        acc[f][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v[h], acc[f][h], FB, FA, 0, (int)sb[f], 0, (int)sa[h]);
-                    } else {
+                    keep_order();
+#pragma unroll
+                    for (int j = h * H * AT_ONCE / MF; j < (h + 1) * H * AT_ONCE / MF; ++j)
+                        if (j < LOADS) fetch(k + 2, j);
+#pragma unroll
+                    for (int f = 0; f < H; ++f)
+                        acc[H + f][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[f], v[h], acc[H + f][h], FB, FA, 0, (int)sb[H + f], 0, (int)sa[h]);
+                    keep_order();
+                    v[h] = codes_a(next, h);
+                }
+            } else {
+#pragma unroll
+                for (int f = 0; f < NF; ++f) {
+                    if (f + 1 == NF) wait_and_meet();
+                    const i8 un = f + 1 < NF ? codes_b(stage, f + 1) : codes_b(next, 0);
+                    keep_order();
+#pragma unroll
+                    for (int j = f * AT_ONCE; j < (f + 1) * AT_ONCE; ++j)
+                        if (j < LOADS) fetch(k + 1, j);
+                    b8 x[4];
+                    widen<FB>(u, sb[f] & 255u, x);
+#pragma unroll
+                    for (int h = 0; h < MF; ++h) {
 #pragma unroll
                         for (int q = 0; q < 4; ++q) acc[f][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[q], wide[h][q], acc[f][h], 0, 0, 0);
+                        if (f + 1 == NF) {
+                            keep_order();
+                            v[h] = codes_a(next, h);
+                            keep_order();
+                        }
                     }
-                    if (f + 1 == NF) {
-                        keep_order();
-                        v[h] = codes_a(next, h);
-                        keep_order();
-                    }
+                    keep_order();
+                    u = un;
                 }
-                keep_order();
-                u = un;
             }
             scales(k + 1);
             const int shift = ((k + 1) & 3) * 8;
@@ -517,49 +572,57 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
                 for (int h = 0; h < MF; ++h) widen<FA>(v[h], sa[h] & 255u, wide[h]);
             }
         }
-        // The next tile's first block is on its way, into stage 0, while this tile's result leaves through stage 1: sixteen rows at a time, so that a
-        // wavefront stores whole stretches of 256 bytes; each has a place of its own, and waits for nobody.
+        // The next tile's first blocks are on their way while this tile's result leaves through LDS, eight rows at a time, so that a wavefront stores whole
+        // stretches of 256 bytes; each has a place of its own, and waits for nobody.
         wait_and_meet();
         const int64_t m_out = m0 + wm * MF * 16 + lane / VECS, n_out = n0 + wn * NF * 16 + (lane % VECS) * PER_VEC;
-        const bool whole = m_here == TM && n_here == TN;
+        const bool whole = m_here == TM && n_here == TN && !p.c_in;
         tile += gridDim.x;
         if (tile < tiles) {
             turn_to(tile);
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) fetch(0, j);
+#pragma unroll
+            for (int j = 0; j < (BF16 ? LOADS : 0); ++j) fetch(1, j);
         }
-        uint8_t* const mine = lds + STAGE + wave * 16 * PITCH;
+        uint8_t* const mine = lds + T::RESULT + wave * 8 * PITCH;
 #pragma unroll
         for (int h = 0; h < MF; ++h) {
 #pragma unroll
             for (int e = 0; e < NF; e += EF) {
 #pragma unroll
-                for (int f = e; f < e + EF; ++f) {
-                    if constexpr (BF16) {
-                        if (f & 1) {
-                            const u4 w = {narrow2(acc[f - 1][h].x, acc[f - 1][h].y), narrow2(acc[f - 1][h].z, acc[f - 1][h].w),
-                                          narrow2(acc[f][h].x, acc[f][h].y), narrow2(acc[f][h].z, acc[f][h].w)};
-                            *reinterpret_cast<u4*>(mine + i * PITCH + ((f >> 1) * 32 + g * 8) * 2) = w;
+                for (int half = 0; half < 2; ++half) {
+                    if ((i >> 3) == half) {
+#pragma unroll
+                        for (int f = e; f < e + EF; ++f) {
+                            if constexpr (BF16) {
+                                if (f & 1) {
+                                    const u4 w = {narrow2(acc[f - 1][h].x, acc[f - 1][h].y), narrow2(acc[f - 1][h].z, acc[f - 1][h].w),
+                                                  narrow2(acc[f][h].x, acc[f][h].y), narrow2(acc[f][h].z, acc[f][h].w)};
+                                    *reinterpret_cast<u4*>(mine + (i & 7) * PITCH + ((f >> 1) * 32 + g * 8) * 2) = w;
+                                }
+                            } else {
+                                *reinterpret_cast<f4*>(mine + (i & 7) * PITCH + ((f - e) * 16 + g * 4) * 4) = acc[f][h];
+                            }
                         }
-                    } else {
-                        *reinterpret_cast<f4*>(mine + i * PITCH + ((f - e) * 16 + g * 4) * 4) = acc[f][h];
                     }
-                }
-                __builtin_amdgcn_wave_barrier();
-                Vec out[16 / TURN];
+                    __builtin_amdgcn_wave_barrier();
+                    Vec out[8 / TURN];
 #pragma unroll
-                for (int t = 0; t < 16 / TURN; ++t) out[t] = *reinterpret_cast<const Vec*>(mine + (t * TURN + lane / VECS) * PITCH + (lane % VECS) * 16);
+                    for (int t = 0; t < 8 / TURN; ++t) out[t] = *reinterpret_cast<const Vec*>(mine + (t * TURN + lane / VECS) * PITCH + (lane % VECS) * 16);
 #pragma unroll
-                for (int t = 0; t < 16 / TURN; ++t) {
-                    const int64_t m = m_out + h * 16 + t * TURN;
-                    if (m < p.M) store_row<BF16>(p, m, n_out + e * 16, out[t]);
+                    for (int t = 0; t < 8 / TURN; ++t) {
+                        const int64_t m = m_out + h * 16 + half * 8 + t * TURN;
+                        if (m < p.M) store_row<BF16>(p, m, n_out + e * 16, out[t]);
+                    }
+                    __builtin_amdgcn_wave_barrier();
                 }
-                __builtin_amdgcn_wave_barrier();
             }
         }
         if (tile >= tiles) return;
         // the loads are older than the stores: where every store was made, these may still be on their way
-        if (whole && !p.c_in) wait_and_meet<STORES>();
+        behind = whole;
+        if (whole) wait_and_meet<(BF16 ? LOADS : 0) + STORES>();
         else wait_and_meet();
     }
 #endif
@@ -596,10 +659,10 @@ void launch_quantize(Quantize p, int64_t tiles, hipStream_t stream)
 template <int FA, int FB, bool BF16, int WN, int WM, int NF, int MF, int PER_SIMD>
 void launch_tiles(Matmul p, hipStream_t stream)
 {
-    constexpr int TN = 16 * WN * NF, TM = 16 * WM * MF;
-    p.n_tiles = (p.N + TN - 1) / TN;
-    p.m_tiles = (p.M + TM - 1) / TM;
-    const int lds = 2 * (TN + TM) * (kBlock + 4) + 256;
+    typedef Tile<BF16, WN, WM, NF, MF> T;
+    p.n_tiles = (p.N + T::TN - 1) / T::TN;
+    p.m_tiles = (p.M + T::TM - 1) / T::TM;
+    const int lds = T::LDS;
     const auto kernel = tile_kernel<FA, FB, BF16, WN, WM, NF, MF, PER_SIMD>;
     const int64_t tiles = p.m_tiles * p.n_tiles, most = (int64_t)compute_units() * (160 * 1024 / lds);      // as many work-groups as there is room for
     hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles < most ? tiles : most)), dim3(64 * WN * WM), lds, stream, p);
