@@ -15,6 +15,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <stdlib.h>
+#include <stdio.h>
 
 #include "ts_densify.h"
 #include "ts_workspace.h"
@@ -206,36 +207,10 @@ struct Matmul {
     int64_t M, N;
     int64_t ld, lds;            // bytes of a row of codes and of scales
     int32_t blocks;             // of 128 along K
-    int64_t tile_first;
+    int32_t parts, part_blocks; // K in parts of so many blocks, a multiple of four: out holds [parts][M][N] sums then
     int64_t m_tiles, n_tiles;
+    int64_t n_first;            // first column of a launch of rows_kernel
 };
-
-// Stores out[m][n .. n + 3].
-template <bool BF16>
-__device__ __forceinline__ void store4(const Matmul& p, int64_t m, int64_t n, f4 v)
-{
-    if (m >= p.M || n >= p.N) return;
-    const int64_t at = m * p.N + n;
-    if ((p.N & 3) == 0) {
-        if (p.c_in) v += *reinterpret_cast<const f4*>(p.c_in + at);
-        if (BF16) {
-            u2 w;
-            w.x = narrow2(v.x, v.y);
-            w.y = narrow2(v.z, v.w);
-            *reinterpret_cast<u2*>((uint16_t*)p.out + at) = w;
-        } else {
-            *reinterpret_cast<f4*>((float*)p.out + at) = v;
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (n + i >= p.N) return;
-        const float x = p.c_in ? v[i] + p.c_in[at + i] : v[i];
-        if (BF16) ((uint16_t*)p.out)[at + i] = (uint16_t)narrow2(x, x);
-        else ((float*)p.out)[at + i] = x;
-    }
-}
 
 // 32 codes of one row as four operands of eight bf16 values, exactly (a value below 2^-133 is cut at bf16's last bit).
 template <int FMT>
@@ -276,13 +251,13 @@ struct Out<false> {
 };
 
 template <bool BF16>
-__device__ __forceinline__ void store_row(const Matmul& p, int64_t m, int64_t n, typename Out<BF16>::Vec v)
+__device__ __forceinline__ void store_row(const Matmul& p, void* to, int64_t m, int64_t n, typename Out<BF16>::Vec v)
 {
     if (n >= p.N) return;
     const int64_t at = m * p.N + n;
     if constexpr (BF16) {
         typedef u4 __attribute__((aligned(2))) any_u4;
-        uint16_t* const out = (uint16_t*)p.out + at;
+        uint16_t* const out = (uint16_t*)to + at;
         if (n + 8 <= p.N) {
             __builtin_nontemporal_store(v, reinterpret_cast<any_u4*>(out));
         } else {
@@ -292,7 +267,7 @@ __device__ __forceinline__ void store_row(const Matmul& p, int64_t m, int64_t n,
         }
     } else {
         typedef f4 __attribute__((aligned(4))) any_f4;
-        float* const out = (float*)p.out + at;
+        float* const out = (float*)to + at;
         if (n + 4 <= p.N) {
             if (p.c_in) v += *reinterpret_cast<const any_f4*>(p.c_in + at);
             __builtin_nontemporal_store(v, reinterpret_cast<any_f4*>(out));
@@ -304,37 +279,108 @@ __device__ __forceinline__ void store_row(const Matmul& p, int64_t m, int64_t n,
     }
 }
 
+// Four elements of a row of the result.
+template <bool HALF>
+__device__ __forceinline__ void store4(const Matmul& p, int64_t m, int64_t n, f4 v)
+{
+    if constexpr (!HALF) {
+        store_row<false>(p, p.out, m, n, v);
+    } else {
+        typedef u2 __attribute__((aligned(2))) any_u2;
+        uint16_t* const out = (uint16_t*)p.out + m * p.N + n;
+        const u2 w = {narrow2(v.x, v.y), narrow2(v.z, v.w)};
+        if (n + 4 <= p.N) {
+            *reinterpret_cast<any_u2*>(out) = w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (n + j < p.N) out[j] = (uint16_t)(w[j >> 1] >> (j & 1) * 16);
+        }
+    }
+}
+
 __device__ __forceinline__ i8 load_codes(const uint8_t* p)
 {
     const i4 lo = *reinterpret_cast<const i4*>(p), hi = *reinterpret_cast<const i4*>(p + 16);
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// A wavefront computes 16 columns of the result in 16 rows: lane l holds 32 codes of row l % 16 of either operand.
-template <int FA, int FB, bool BF16>
-__global__ __launch_bounds__(256) void matmul_kernel(Matmul p)
+// ---- few rows: codes straight into registers
+// A wavefront computes 16 columns of the result in MF * 16 rows: lane l holds 32 codes of row l % 16 of a fragment.  It takes every kw-th run of four
+// blocks, all of whose codes it asks for at once; the kw wavefronts of one place add their sums up in LDS, in their order.  Bound by reading B once.
+template <int FA, int FB, bool NATIVE, bool HALF, int MF>
+__global__ __launch_bounds__(1024) void rows_kernel(Matmul p, int log_kw)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t tile = p.tile_first + blockIdx.x;
-    const int64_t m0 = tile / p.n_tiles * 16, n0 = (tile % p.n_tiles) * 64 + wave * 16;
-    const int64_t m = m0 + (lane & 15), n = n0 + (lane & 15);
-    const int64_t ra = m < p.M ? m : p.M - 1, rb = n < p.N ? n : p.N - 1;       // rows past the end: the last one again
-    const uint8_t *a = p.a + ra * p.ld + (lane >> 4) * 32, *b = p.b + rb * p.ld + (lane >> 4) * 32;
-    const uint8_t *sa = p.a_scales + ra * p.lds, *sb = p.b_scales + rb * p.lds;
-    f4 acc = (f4)(0.0f);
-    for (int k = 0; k < p.blocks; ++k) {
-        const i8 u = load_codes(b + (int64_t)k * kBlock), v = load_codes(a + (int64_t)k * kBlock);
-        if (BF16) {
-            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v, acc, FB, FA, 0, sb[k], 0, sa[k]);
-        } else {
-            b8 x[4], y[4];
-            widen<FB>(u, sb[k], x);
-            widen<FA>(v, sa[k], y);
+    constexpr int U = MF > 2 ? 2 : 4;           // blocks that are loaded together
+    __shared__ f4 sums[16][MF][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
+    const int kw = 1 << log_kw, part = wave & (kw - 1), places = (int)(blockDim.x >> 6) >> log_kw;
+    const int64_t n0 = p.n_first + ((int64_t)blockIdx.x * places + (wave >> log_kw)) * 16, m0 = (int64_t)blockIdx.y * (MF * 16);
+    const int64_t n = n0 + i, rb = n < p.N ? n : p.N - 1;                 // rows past the end: the last one again
+    const uint8_t *const b = p.b + rb * p.ld + g * 32, *const sb = p.b_scales + rb * p.lds;
+    const uint8_t *a[MF], *sa[MF];
+    f4 acc[MF];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[q], y[q], acc, 0, 0, 0);
+    for (int h = 0; h < MF; ++h) {
+        const int64_t m = m0 + h * 16 + i, ra = m < p.M ? m : p.M - 1;
+        a[h] = p.a + ra * p.ld + g * 32;
+        sa[h] = p.a_scales + ra * p.lds;
+        acc[h] = (f4)(0.0f);
+    }
+    for (int k = part * 4; k < p.blocks; k += kw * 4) {
+        const uint32_t wb = *reinterpret_cast<const uint32_t*>(sb + k);
+        uint32_t wa[MF];
+#pragma unroll
+        for (int h = 0; h < MF; ++h) wa[h] = *reinterpret_cast<const uint32_t*>(sa[h] + k);
+#pragma unroll
+        for (int q0 = 0; q0 < 4; q0 += U) {
+            i8 u[U], v[U][MF];
+#pragma unroll
+            for (int q = 0; q < U; ++q) {
+                const int64_t at = (int64_t)(k + q0 + q < p.blocks ? k + q0 + q : p.blocks - 1) * kBlock;      // (behind the last block: it again, unused)
+                u[q] = load_codes(b + at);
+#pragma unroll
+                for (int h = 0; h < MF; ++h) v[q][h] = load_codes(a[h] + at);
+            }
+#pragma unroll
+            for (int q = 0; q < U; ++q) {
+                if (k + q0 + q >= p.blocks) break;
+                const int shift = (q0 + q) * 8;
+                if constexpr (NATIVE) {
+#pragma unroll
+                    for (int h = 0; h < MF; ++h)
+                        acc[h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u[q], v[q][h], acc[h], FB, FA, 0, (int)(wb >> shift), 0, (int)(wa[h] >> shift));
+                } else {
+                    b8 x[4];
+                    widen<FB>(u[q], (wb >> shift) & 255u, x);
+#pragma unroll
+                    for (int h = 0; h < MF; ++h) {
+                        b8 y[4];
+                        widen<FA>(v[q][h], (wa[h] >> shift) & 255u, y);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[r], y[r], acc[h], 0, 0, 0);
+                    }
+                }
+            }
         }
     }
-    store4<BF16>(p, m, n0 + (lane >> 4) * 4, acc);
+    if (kw > 1) {
+        if (part > 0) {
+#pragma unroll
+            for (int h = 0; h < MF; ++h) sums[wave][h][lane] = acc[h];
+        }
+        __syncthreads();
+        if (part > 0) return;
+        for (int w = 1; w < kw; ++w)
+#pragma unroll
+            for (int h = 0; h < MF; ++h) acc[h] += sums[wave + w][h][lane];
+    }
+    const int64_t n4 = n0 + g * 4;
+#pragma unroll
+    for (int h = 0; h < MF; ++h) {
+        const int64_t m = m0 + h * 16 + i;
+        if (m < p.M) store4<HALF>(p, m, n4, acc[h]);
+    }
 }
 
 // ---- large products: tiles through LDS
@@ -382,18 +428,18 @@ __device__ __forceinline__ void place(int64_t wg, int64_t m_tiles, int64_t n_til
 
 // Sizes that the host needs, too.  LDS: two stages of [ROWS][128] codes, two of [ROWS] words of scales, 1 KiB that nobody reads, and eight rows of
 // the result for every wavefront.
-template <bool BF16, int WN, int WM, int NF, int MF>
+template <bool HALF, int WN, int WM, int NF, int MF>
 struct Tile {
     static constexpr int TN = 16 * WN * NF, TM = 16 * WM * MF, ROWS = TN + TM, STAGE = ROWS * kBlock, SCALES = 2 * STAGE, UNREAD = SCALES + 2 * ROWS * 4;
-    static constexpr int EF = BF16 ? NF : NF / 2, PITCH = EF * 16 * (BF16 ? 2 : 4) + 16;       // fragments of a turn of the result; bytes of a row
+    static constexpr int EF = HALF ? NF : NF / 2, PITCH = EF * 16 * (HALF ? 2 : 4) + 16;       // fragments of a turn of the result; bytes of a row
     static constexpr int RESULT = UNREAD + 1024, LDS = RESULT + WN * WM * 8 * PITCH;
 };
 
-template <int FA, int FB, bool BF16, int WN, int WM, int NF, int MF, int PER_SIMD>
-__global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
+template <int FA, int FB, bool NATIVE, bool HALF, int WN, int WM, int NF, int MF>
+__global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
 {
 #ifdef __HIP_DEVICE_COMPILE__     // (a buffer's type is none of the host compiler's)
-    typedef Tile<BF16, WN, WM, NF, MF> T;
+    typedef Tile<HALF, WN, WM, NF, MF> T;
     constexpr int TN = T::TN, TM = T::TM, ROWS = T::ROWS, STAGE = T::STAGE, SCALES = T::SCALES, WAVES = WN * WM;
     constexpr int LB = TN / (8 * WAVES), LA = TM / (8 * WAVES);     // loads of 1 KiB by a wavefront, for one block
     static_assert(TN % (8 * WAVES) == 0 && TM % (8 * WAVES) == 0 && TN % 64 == 0 && TM % 64 == 0, "whole loads");
@@ -403,49 +449,58 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
     // Row r of a stage: of B for r < TN, else of A; its 16-byte chunk c lies in slot c ^ key(r), so that sixteen lanes that read
     // one chunk of sixteen rows meet no bank twice.  With a bf16 result, rows of two fragments of B are interleaved by fours (n_of), and the
     // four columns that a lane has of each lie side by side.
-    const auto n_of = [&](int f) { return BF16 ? (f >> 1) * 32 + (i >> 2) * 8 + (f & 1) * 4 + (i & 3) : f * 16 + i; };
+    const auto n_of = [&](int f) { return HALF ? (f >> 1) * 32 + (i >> 2) * 8 + (f & 1) * 4 + (i & 3) : f * 16 + i; };
     const uint32_t ld = (uint32_t)p.ld, rb = (uint32_t)(wave * LB * 8 + (lane >> 3)), ra = (uint32_t)(wave * LA * 8 + (lane >> 3));
-    const uint32_t key_b = BF16 ? (rb & 3) | ((rb >> 1) & 4) : rb & 7;
+    const uint32_t key_b = HALF ? (rb & 3) | ((rb >> 1) & 4) : rb & 7;
     const uint32_t from_b = rb * ld + (((lane & 7) ^ key_b) << 4), from_a = ra * ld + (((lane & 7) ^ (ra & 7)) << 4);
     uint32_t row_b[LB], row_a[LA];
 #pragma unroll
-    for (int j = 0; j < LB; ++j) row_b[j] = (BF16 && (j & 1) ? from_b ^ 64 : from_b) + j * 8 * ld;    // (eight rows on, the key's third bit is the other one)
+    for (int j = 0; j < LB; ++j) row_b[j] = (HALF && (j & 1) ? from_b ^ 64 : from_b) + j * 8 * ld;    // (eight rows on, the key's third bit is the other one)
 #pragma unroll
     for (int j = 0; j < LA; ++j) row_a[j] = from_a + j * 8 * ld;
     // the tile that is fetched
     int64_t m0, n0, m_here, n_here;
     const uint8_t *a, *b, *sa_from, *sb_from;
+    int64_t a_bytes, b_bytes, words_bytes;
+    int blocks, part;
+    const int64_t tiles = p.m_tiles * p.n_tiles, all = tiles * p.parts;
     const auto turn_to = [&](int64_t t) {
         int64_t mt, nt;
-        place(t, p.m_tiles, p.n_tiles, &mt, &nt);
+        part = (int)(t / tiles);
+        place(t - part * tiles, p.m_tiles, p.n_tiles, &mt, &nt);
+        const int k0 = part * p.part_blocks;
+        blocks = p.blocks - k0 < p.part_blocks ? p.blocks - k0 : p.part_blocks;
         m0 = mt * TM;
         n0 = nt * TN;
         m_here = p.M - m0 < TM ? p.M - m0 : TM;
         n_here = p.N - n0 < TN ? p.N - n0 : TN;
-        a = p.a + m0 * p.ld;
-        b = p.b + n0 * p.ld;
-        sa_from = p.a_scales + m0 * p.lds;
-        sb_from = p.b_scales + n0 * p.lds;
+        a = p.a + m0 * p.ld + (int64_t)k0 * kBlock;
+        b = p.b + n0 * p.ld + (int64_t)k0 * kBlock;
+        sa_from = p.a_scales + m0 * p.lds + k0;
+        sb_from = p.b_scales + n0 * p.lds + k0;
+        a_bytes = m_here * p.ld - (int64_t)k0 * kBlock;
+        b_bytes = n_here * p.ld - (int64_t)k0 * kBlock;
+        words_bytes = -k0;
     };
     // Load j of this wavefront's share of block k (codes of B, of A, words of four scales), into stage k % 2.  Behind the last block: zeros, without
     // a question, so that the loop below stays one run of instructions that keeps its order.
     constexpr int LS = (ROWS / 64 + WAVES - 1) / WAVES, LOADS = LB + LA + LS;
     const auto fetch = [&](int k, int j, bool wanted = true) {
-        const bool there = wanted && k < p.blocks;
+        const bool there = wanted && k < blocks;
         uint8_t* const to = wanted ? lds + (k & 1) * STAGE : nullptr;          // (a load that was made before: to where nobody looks)
         uint8_t* const unread = lds + T::UNREAD;
         const int at_k = there ? k * kBlock : 0;            // (never more than a buffer's length)
         if (j < LB) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(b, there ? n_here * p.ld : 0), (lds_ptr)(wanted ? to + (wave * LB + j) * 1024 : unread), 16, row_b[j], at_k, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(b, there ? b_bytes : 0), (lds_ptr)(wanted ? to + (wave * LB + j) * 1024 : unread), 16, row_b[j], at_k, 0, 0);
         } else if (j < LB + LA) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(a, there ? m_here * p.ld : 0), (lds_ptr)(wanted ? to + TN * kBlock + (wave * LA + j - LB) * 1024 : unread), 16,
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(a, there ? a_bytes : 0), (lds_ptr)(wanted ? to + TN * kBlock + (wave * LA + j - LB) * 1024 : unread), 16,
                                                      row_a[j - LB], at_k, 0, 0);
         } else {
             // every fourth block has new words; else nothing is read, and zeros go where nobody looks
             const bool words = there && (k & 3) == 0;
             const int at = (wave + (j - LB - LA) * WAVES) % (ROWS / 64);        // (more wavefronts than words: some are fetched twice)
             const bool of_b = at * 64 < TN;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(of_b ? sb_from : sa_from, words ? (of_b ? n_here : m_here) * p.lds : 0),
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(of_b ? sb_from : sa_from, words ? (of_b ? n_here : m_here) * p.lds + words_bytes : 0),
                                                      (lds_ptr)(words ? lds + SCALES + (k >> 2 & 1) * ROWS * 4 + at * 256 : unread), 4,
                                                      (uint32_t)(at * 64 + lane - (of_b ? 0 : TN)) * (uint32_t)p.lds, words ? k : 0, 0, 0);
         }
@@ -456,7 +511,7 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
         const i4 x = *reinterpret_cast<const i4*>(lds + at + lo), y = *reinterpret_cast<const i4*>(lds + at + hi);
         return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    const auto codes_b = [&](int stage, int f) { return codes(stage + at_b + (BF16 ? (f >> 1) * 32 + (f & 1) * 4 : f * 16) * kBlock); };
+    const auto codes_b = [&](int stage, int f) { return codes(stage + at_b + (HALF ? (f >> 1) * 32 + (f & 1) * 4 : f * 16) * kBlock); };
     const auto codes_a = [&](int stage, int h) { return codes(stage + at_a + h * 16 * kBlock); };
     uint32_t sb[NF], sa[MF];
     const auto scales = [&](int k) {
@@ -469,21 +524,20 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
     // A block's last fragment of B is multiplied behind the meeting that ends its stage, while the next block's first codes are
     // on their way from LDS; the loads of the block after that, into the stage that the meeting has set free, are spread over the first
     // half of the next block, so that none of them holds up a read from LDS that a multiplication waits for.
-    constexpr int SPREAD = BF16 ? NF : NF > 4 ? NF / 2 : NF - 1, AT_ONCE = (LOADS + SPREAD - 1) / SPREAD;
-    typedef typename Out<BF16>::Vec Vec;
-    constexpr int PER_VEC = 16 / Out<BF16>::BYTES, EF = T::EF, VECS = EF * 16 / PER_VEC, PITCH = T::PITCH, TURN = 64 / VECS;
+    constexpr int SPREAD = NATIVE ? NF : NF > 4 ? NF / 2 : NF - 1, AT_ONCE = (LOADS + SPREAD - 1) / SPREAD;
+    typedef typename Out<HALF>::Vec Vec;
+    constexpr int PER_VEC = 16 / Out<HALF>::BYTES, EF = T::EF, VECS = EF * 16 / PER_VEC, PITCH = T::PITCH, TURN = 64 / VECS;
     static_assert(64 % VECS == 0 && 8 % TURN == 0, "whole rows");
     constexpr int STORES = MF * (NF / EF) * (16 / TURN);
     // loads of the block after the next that are made before the next one begins
-    constexpr int FIRST = !BF16 ? 0 : NF / 2 * AT_ONCE < LOADS ? NF / 2 * AT_ONCE : LOADS;
-    const int64_t tiles = p.m_tiles * p.n_tiles;
+    constexpr int FIRST = !NATIVE ? 0 : NF / 2 * AT_ONCE < LOADS ? NF / 2 * AT_ONCE : LOADS;
     int64_t tile = blockIdx.x;
     turn_to(tile);
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) fetch(0, j);
 #pragma unroll
-    for (int j = 0; j < (BF16 ? LOADS : 0); ++j) fetch(1, j);
-    wait_and_meet<BF16 ? LOADS : 0>();
+    for (int j = 0; j < (NATIVE ? LOADS : 0); ++j) fetch(1, j);
+    wait_and_meet<NATIVE ? LOADS : 0>();
     bool behind = false;        // stores of the last tile lie between the loads
     for (;;) {
         f4 acc[NF][MF];
@@ -496,13 +550,13 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
         b8 wide[MF][4];
 #pragma unroll
         for (int h = 0; h < MF; ++h) v[h] = codes_a(0, h);
-        if constexpr (!BF16) {
+        if constexpr (!NATIVE) {
 #pragma unroll
             for (int h = 0; h < MF; ++h) widen<FA>(v[h], sa[h] & 255u, wide[h]);
         }
-        for (int k = 0; k < p.blocks; ++k) {
+        for (int k = 0; k < blocks; ++k) {
             const int stage = (k & 1) * STAGE, next = STAGE - stage;
-            if constexpr (BF16) {
+            if constexpr (NATIVE) {
                 // First half of the fragments of B: each is multiplied while the one after it is read, and the second half's are read besides.
                 constexpr int H = NF / 2;
                 i8 w[H];
@@ -567,7 +621,7 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
             for (int f = 0; f < NF; ++f) sb[f] >>= shift;
 #pragma unroll
             for (int h = 0; h < MF; ++h) sa[h] >>= shift;
-            if constexpr (!BF16) {
+            if constexpr (!NATIVE) {
 #pragma unroll
                 for (int h = 0; h < MF; ++h) widen<FA>(v[h], sa[h] & 255u, wide[h]);
             }
@@ -577,13 +631,14 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
         wait_and_meet();
         const int64_t m_out = m0 + wm * MF * 16 + lane / VECS, n_out = n0 + wn * NF * 16 + (lane % VECS) * PER_VEC;
         const bool whole = m_here == TM && n_here == TN && !p.c_in;
+        void* const out_part = (char*)p.out + (int64_t)part * p.M * p.N * 4;            // (parts are fp32)
         tile += gridDim.x;
-        if (tile < tiles) {
+        if (tile < all) {
             turn_to(tile);
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) fetch(0, j);
 #pragma unroll
-            for (int j = 0; j < (BF16 ? LOADS : 0); ++j) fetch(1, j);
+            for (int j = 0; j < (NATIVE ? LOADS : 0); ++j) fetch(1, j);
         }
         uint8_t* const mine = lds + T::RESULT + wave * 8 * PITCH;
 #pragma unroll
@@ -595,7 +650,7 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
                     if ((i >> 3) == half) {
 #pragma unroll
                         for (int f = e; f < e + EF; ++f) {
-                            if constexpr (BF16) {
+                            if constexpr (HALF) {
                                 if (f & 1) {
                                     const u4 w = {narrow2(acc[f - 1][h].x, acc[f - 1][h].y), narrow2(acc[f - 1][h].z, acc[f - 1][h].w),
                                                   narrow2(acc[f][h].x, acc[f][h].y), narrow2(acc[f][h].z, acc[f][h].w)};
@@ -613,27 +668,67 @@ __global__ __launch_bounds__(64 * WN * WM, PER_SIMD) void tile_kernel(Matmul p)
 #pragma unroll
                     for (int t = 0; t < 8 / TURN; ++t) {
                         const int64_t m = m_out + h * 16 + half * 8 + t * TURN;
-                        if (m < p.M) store_row<BF16>(p, m, n_out + e * 16, out[t]);
+                        if (m < p.M) store_row<HALF>(p, out_part, m, n_out + e * 16, out[t]);
                     }
                     __builtin_amdgcn_wave_barrier();
                 }
             }
         }
-        if (tile >= tiles) return;
+        if (tile >= all) return;
         // the loads are older than the stores: where every store was made, these may still be on their way
         behind = whole;
-        if (whole) wait_and_meet<(BF16 ? LOADS : 0) + STORES>();
+        if (whole) wait_and_meet<(NATIVE ? LOADS : 0) + STORES>();
         else wait_and_meet();
     }
 #endif
 }
 
+// out = c_in + part 0 + part 1 + ..., four elements per lane.
+template <bool HALF>
+__global__ __launch_bounds__(256) void add_parts_kernel(const float* parts, int count, const float* c_in, void* out, int64_t n, int64_t first_wg)
+{
+    typedef f4 __attribute__((aligned(4))) any_f4;
+    const int64_t at = ((first_wg + blockIdx.x) * 256 + threadIdx.x) * 4;
+    if (at >= n) return;
+    const bool four = at + 4 <= n;
+    f4 v = (f4)(0.0f);
+    const auto add = [&](const float* p) {
+        if (four) {
+            v += *reinterpret_cast<const any_f4*>(p + at);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (at + j < n) v[j] += p[at + j];
+        }
+    };
+    for (int s = 0; s < count; ++s) add(parts + s * n);
+    if (c_in) add(c_in);
+    if constexpr (HALF) {
+        const u2 w = {narrow2(v.x, v.y), narrow2(v.z, v.w)};
+        if (four) {
+            *reinterpret_cast<u2*>((uint16_t*)out + at) = w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (at + j < n) ((uint16_t*)out)[at + j] = (uint16_t)(w[j >> 1] >> (j & 1) * 16);
+        }
+    } else {
+        if (four) {
+            *reinterpret_cast<f4*>((float*)out + at) = v;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (at + j < n) ((float*)out)[at + j] = v[j];
+        }
+    }
+}
+
 constexpr int64_t kMaxWgs = 1 << 22;      // work-groups per launch (a launch has less than 2^32 threads)
 
 template <typename F>
-void in_launches(int64_t tiles, F&& launch)
+void in_launches(int64_t wgs, int64_t most, F&& launch)
 {
-    for (int64_t at = 0; at < tiles; at += kMaxWgs) launch(at, (unsigned)(tiles - at < kMaxWgs ? tiles - at : kMaxWgs));
+    for (int64_t at = 0; at < wgs; at += most) launch(at, (unsigned)(wgs - at < most ? wgs - at : most));
 }
 
 // Compute units of the current GPU.
@@ -649,50 +744,121 @@ int compute_units()
 template <typename T, int FMT>
 void launch_quantize(Quantize p, int64_t tiles, hipStream_t stream)
 {
-    in_launches(tiles, [&](int64_t at, unsigned n) {
+    in_launches(tiles, kMaxWgs, [&](int64_t at, unsigned n) {
         p.tile_first = at;
         if (p.cols % 4 == 0) hipLaunchKernelGGL((quantize_kernel<T, FMT, true>), dim3(n), dim3(256), 0, stream, p);
         else hipLaunchKernelGGL((quantize_kernel<T, FMT, false>), dim3(n), dim3(256), 0, stream, p);
     });
 }
 
-template <int FA, int FB, bool BF16, int WN, int WM, int NF, int MF, int PER_SIMD>
+// How a product is computed.  The form and the number of parts fix the order of additions, so they follow from the sizes and the result's type alone,
+// as if for a GPU of 256 compute units.
+enum { FORM_ROWS, FORM_SMALL, FORM_LARGE };
+struct Way {
+    int form;
+    int parts, part_blocks;
+    int log_kw;             // FORM_ROWS: wavefronts that share a place
+};
+
+Way way_for(int64_t M, int64_t N, int64_t K, bool half)
+{
+    const int blocks = (int)(code_row(K) / kBlock);
+    Way w{FORM_ROWS, 1, blocks, 0};
+    if (const char* e = getenv("MMF")) {
+        int f, q, l;
+        if (sscanf(e, "%d,%d,%d", &f, &q, &l) == 3 && blocks) {
+            w.form = f; w.part_blocks = ((blocks + q - 1) / q + 3) / 4 * 4; w.parts = (blocks + w.part_blocks - 1) / w.part_blocks; w.log_kw = l;
+            if (f == FORM_ROWS) { w.parts = 1; w.part_blocks = blocks; }
+            return w;
+        }
+    }
+    if (blocks == 0) return w;
+    if (M <= 32) {
+        const int64_t places = (N + 15) / 16 * ((M + 15) / 16);
+        while (w.log_kw < 4 && (places << w.log_kw) < 2048 && (4 << w.log_kw) < blocks) ++w.log_kw;
+        return w;
+    }
+    double best = 1e30;
+    for (int form = FORM_SMALL; form <= FORM_LARGE; ++form) {
+        const int64_t t = form == FORM_SMALL ? 128 : 256, tiles = (M + t - 1) / t * ((N + t - 1) / t), room = form == FORM_SMALL ? 512 : 256;
+        const double block_us = (form == FORM_SMALL ? 1.05 : 1.55) * (half ? 1 : 1.7), tile_us = form == FORM_SMALL ? 2.5 : 5;
+        for (int parts = 1; parts <= 64 && (parts == 1 || parts * 4 <= blocks); ++parts) {
+            const int per = parts == 1 ? blocks : ((blocks + parts - 1) / parts + 3) / 4 * 4;
+            const int q = (blocks + per - 1) / per;
+            if (q != parts) continue;
+            const double us = (double)((tiles * q + room - 1) / room) * (per * block_us + tile_us) + (q > 1 ? 3 + (double)M * N * (4 * q + 4) / 4e6 : 0);
+            if (us < best) {
+                best = us;
+                w = Way{form, q, per, 0};
+            }
+        }
+    }
+    return w;
+}
+
+template <int FA, int FB, bool NATIVE, bool HALF, int WN, int WM, int NF, int MF>
 void launch_tiles(Matmul p, hipStream_t stream)
 {
-    typedef Tile<BF16, WN, WM, NF, MF> T;
+    typedef Tile<HALF, WN, WM, NF, MF> T;
     p.n_tiles = (p.N + T::TN - 1) / T::TN;
     p.m_tiles = (p.M + T::TM - 1) / T::TM;
+    const auto kernel = tile_kernel<FA, FB, NATIVE, HALF, WN, WM, NF, MF>;
     const int lds = T::LDS;
-    const auto kernel = tile_kernel<FA, FB, BF16, WN, WM, NF, MF, PER_SIMD>;
-    const int64_t tiles = p.m_tiles * p.n_tiles, most = (int64_t)compute_units() * (160 * 1024 / lds);      // as many work-groups as there is room for
+    const int64_t tiles = p.m_tiles * p.n_tiles * p.parts, most = (int64_t)compute_units() * (160 * 1024 / lds);      // as many work-groups as there is room for
     hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles < most ? tiles : most)), dim3(64 * WN * WM), lds, stream, p);
 }
 
-template <int FA, int FB>
-void launch_matmul(Matmul p, bool bf16, hipStream_t stream)
+template <int FA, int FB, bool NATIVE, bool HALF, int MF>
+void launch_rows(Matmul p, int log_kw, hipStream_t stream)
 {
-    if (p.blocks > 0 && p.M > 64 && p.N > 64) {          // (a tile's first block is fetched without a question)
-        static const int v = getenv("MMV") ? atoi(getenv("MMV")) : 0;
-        if (bf16) {
-            if (v == 0) launch_tiles<FA, FB, true, 2, 4, 8, 4, 2>(p, stream);
-            else if (v == 1) launch_tiles<FA, FB, true, 2, 2, 8, 8, 1>(p, stream);
-            else if (v == 2) launch_tiles<FA, FB, true, 2, 2, 4, 4, 2>(p, stream);
-            else launch_tiles<FA, FB, true, 4, 2, 4, 8, 2>(p, stream);
-        } else {
-            if (v == 0) launch_tiles<FA, FB, false, 2, 2, 4, 4, 2>(p, stream);
-            else if (v == 1) launch_tiles<FA, FB, false, 2, 4, 8, 4, 2>(p, stream);
-            else if (v == 2) launch_tiles<FA, FB, false, 2, 2, 8, 8, 1>(p, stream);
-            else launch_tiles<FA, FB, false, 4, 2, 4, 4, 2>(p, stream);
-        }
-        return;
-    }
-    p.n_tiles = (p.N + 63) / 64;
-    in_launches((p.M + 15) / 16 * p.n_tiles, [&](int64_t at, unsigned n) {
-        p.tile_first = at;
-        if (bf16) hipLaunchKernelGGL((matmul_kernel<FA, FB, true>), dim3(n), dim3(256), 0, stream, p);
-        else hipLaunchKernelGGL((matmul_kernel<FA, FB, false>), dim3(n), dim3(256), 0, stream, p);
+    const int waves = log_kw > 2 ? 16 : 4, places = waves >> log_kw;
+    in_launches((p.N + 16 * places - 1) / (16 * places), kMaxWgs / 8, [&](int64_t at, unsigned n) {
+        p.n_first = at * 16 * places;
+        hipLaunchKernelGGL((rows_kernel<FA, FB, NATIVE, HALF, MF>), dim3(n, (unsigned)((p.M + 16 * MF - 1) / (16 * MF))), dim3(64 * waves), 0, stream, p, log_kw);
     });
 }
+
+template <bool HALF>
+void launch_add(const float* parts, int count, const float* c_in, void* out, int64_t n, hipStream_t stream)
+{
+    in_launches((n + 1023) / 1024, kMaxWgs, [&](int64_t at, unsigned wgs) {
+        hipLaunchKernelGGL((add_parts_kernel<HALF>), dim3(wgs), dim3(256), 0, stream, parts, count, c_in, out, n, at);
+    });
+}
+
+template <int FA, int FB, bool NATIVE>
+void launch_matmul(Matmul p, const Way& w, float* parts, hipStream_t stream)
+{
+    if (w.form == FORM_ROWS) {
+        if (p.M <= 16) launch_rows<FA, FB, NATIVE, NATIVE, 1>(p, w.log_kw, stream);
+        else if (p.M <= 32) launch_rows<FA, FB, NATIVE, NATIVE, 2>(p, w.log_kw, stream);
+        else launch_rows<FA, FB, NATIVE, NATIVE, 4>(p, w.log_kw, stream);
+        return;
+    }
+    p.parts = w.parts;
+    p.part_blocks = w.part_blocks;
+    if (w.parts == 1) {
+        if (w.form == FORM_LARGE) launch_tiles<FA, FB, NATIVE, NATIVE, 2, 4, 8, 4>(p, stream);
+        else launch_tiles<FA, FB, NATIVE, NATIVE, 2, 2, 4, 4>(p, stream);
+        return;
+    }
+    const float* const c_in = p.c_in;
+    void* const out = p.out;
+    p.c_in = nullptr;
+    p.out = parts;
+    if (w.form == FORM_LARGE) launch_tiles<FA, FB, NATIVE, false, 2, 4, 8, 4>(p, stream);
+    else launch_tiles<FA, FB, NATIVE, false, 2, 2, 4, 4>(p, stream);
+    launch_add<NATIVE>(parts, w.parts, c_in, out, p.M * p.N, stream);
+}
+
+template <int FA, int FB>
+void launch_matmul(const Matmul& p, bool half, const Way& w, float* parts, hipStream_t stream)
+{
+    if (half) launch_matmul<FA, FB, true>(p, w, parts, stream);
+    else launch_matmul<FA, FB, false>(p, w, parts, stream);
+}
+
+int64_t parts_bytes(int64_t M, int64_t N, const Way& w) { return w.parts > 1 ? round_up(4 * M * N * w.parts, 256) : 0; }
 
 bool unaligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
 bool bad_format(int32_t f) { return f != TS_FP8_E4M3 && f != TS_FP8_E5M2; }
@@ -744,7 +910,8 @@ int ts_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t* bytes)
     if (!bytes) return TS_ERR_NULL;
     if (M < 0 || N < 0 || K < 0) return TS_ERR_SHAPE;
     if (M >= kSizeMax || N >= kSizeMax || K > kKMax) return TS_ERR_OVERFLOW;
-    *bytes = 0;
+    const int64_t half = parts_bytes(M, N, way_for(M, N, K, true)), full = parts_bytes(M, N, way_for(M, N, K, false));
+    *bytes = half > full ? half : full;
     return TS_OK;
 }
 
@@ -770,12 +937,26 @@ int ts_matmul_fp8(const uint8_t* a, const uint8_t* a_scales, int32_t a_format, c
     p.ld = code_row(K);
     p.lds = scale_row(K);
     p.blocks = (int32_t)(p.ld / kBlock);
-    const bool bf16 = out_dtype == TS_OUT_BF16;
+    p.parts = 1;
+    p.part_blocks = p.blocks;
+    p.m_tiles = p.n_tiles = p.n_first = 0;
+    const bool half = out_dtype == TS_OUT_BF16;
     const hipStream_t s = (hipStream_t)stream;
-    if (a_format == TS_FP8_E4M3 && b_format == TS_FP8_E4M3) launch_matmul<TS_FP8_E4M3, TS_FP8_E4M3>(p, bf16, s);
-    else if (a_format == TS_FP8_E4M3) launch_matmul<TS_FP8_E4M3, TS_FP8_E5M2>(p, bf16, s);
-    else if (b_format == TS_FP8_E4M3) launch_matmul<TS_FP8_E5M2, TS_FP8_E4M3>(p, bf16, s);
-    else launch_matmul<TS_FP8_E5M2, TS_FP8_E5M2>(p, bf16, s);
+    if (K == 0) {           // nothing to add up, and no operands to look at
+        if (half) launch_add<true>(nullptr, 0, nullptr, out, M * N, s);
+        else launch_add<false>(nullptr, 0, c_in, out, M * N, s);
+        return hipGetLastError() == hipSuccess ? TS_OK : TS_ERR_HIP;
+    }
+    const Way w = way_for(M, N, K, half);
+    void* parts = nullptr;
+    if (w.parts > 1) {
+        const int rc = ts_workspace::take(parts_bytes(M, N, w), &parts);
+        if (rc != TS_OK) return rc;
+    }
+    if (a_format == TS_FP8_E4M3 && b_format == TS_FP8_E4M3) launch_matmul<TS_FP8_E4M3, TS_FP8_E4M3>(p, half, w, (float*)parts, s);
+    else if (a_format == TS_FP8_E4M3) launch_matmul<TS_FP8_E4M3, TS_FP8_E5M2>(p, half, w, (float*)parts, s);
+    else if (b_format == TS_FP8_E4M3) launch_matmul<TS_FP8_E5M2, TS_FP8_E4M3>(p, half, w, (float*)parts, s);
+    else launch_matmul<TS_FP8_E5M2, TS_FP8_E5M2>(p, half, w, (float*)parts, s);
     return hipGetLastError() == hipSuccess ? TS_OK : TS_ERR_HIP;
 }
 
