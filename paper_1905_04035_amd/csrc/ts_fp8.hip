@@ -14,8 +14,6 @@
 // matrix instructions (16 x 32 by 32 x 16, half the rate), whose products are exact and whose sums are fp32.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
-#include <stdlib.h>
-#include <stdio.h>
 
 #include "ts_densify.h"
 #include "ts_workspace.h"
@@ -207,7 +205,9 @@ struct Matmul {
     int64_t M, N;
     int64_t ld, lds;            // bytes of a row of codes and of scales
     int32_t blocks;             // of 128 along K
-    int32_t parts, part_blocks; // K in parts of so many blocks, a multiple of four: out holds [parts][M][N] sums then
+    int32_t parts, part_blocks; // tiles beyond the first `full` are computed in parts of so many blocks, a multiple of four
+    int64_t full;
+    f4* sums;                   // [parts][those tiles][wavefronts][fragments][64]: the parts' sums as the registers hold them
     int64_t m_tiles, n_tiles;
     int64_t n_first;            // first column of a launch of rows_kernel
 };
@@ -251,13 +251,13 @@ struct Out<false> {
 };
 
 template <bool BF16>
-__device__ __forceinline__ void store_row(const Matmul& p, void* to, int64_t m, int64_t n, typename Out<BF16>::Vec v)
+__device__ __forceinline__ void store_row(const Matmul& p, int64_t m, int64_t n, typename Out<BF16>::Vec v)
 {
     if (n >= p.N) return;
     const int64_t at = m * p.N + n;
     if constexpr (BF16) {
         typedef u4 __attribute__((aligned(2))) any_u4;
-        uint16_t* const out = (uint16_t*)to + at;
+        uint16_t* const out = (uint16_t*)p.out + at;
         if (n + 8 <= p.N) {
             __builtin_nontemporal_store(v, reinterpret_cast<any_u4*>(out));
         } else {
@@ -267,7 +267,7 @@ __device__ __forceinline__ void store_row(const Matmul& p, void* to, int64_t m, 
         }
     } else {
         typedef f4 __attribute__((aligned(4))) any_f4;
-        float* const out = (float*)to + at;
+        float* const out = (float*)p.out + at;
         if (n + 4 <= p.N) {
             if (p.c_in) v += *reinterpret_cast<const any_f4*>(p.c_in + at);
             __builtin_nontemporal_store(v, reinterpret_cast<any_f4*>(out));
@@ -284,7 +284,7 @@ template <bool HALF>
 __device__ __forceinline__ void store4(const Matmul& p, int64_t m, int64_t n, f4 v)
 {
     if constexpr (!HALF) {
-        store_row<false>(p, p.out, m, n, v);
+        store_row<false>(p, m, n, v);
     } else {
         typedef u2 __attribute__((aligned(2))) any_u2;
         uint16_t* const out = (uint16_t*)p.out + m * p.N + n;
@@ -308,21 +308,21 @@ __device__ __forceinline__ i8 load_codes(const uint8_t* p)
 // ---- few rows: codes straight into registers
 // A wavefront computes 16 columns of the result in MF * 16 rows: lane l holds 32 codes of row l % 16 of a fragment.  It takes every kw-th run of four
 // blocks, all of whose codes it asks for at once; the kw wavefronts of one place add their sums up in LDS, in their order.  Bound by reading B once.
-template <int FA, int FB, bool NATIVE, bool HALF, int MF>
-__global__ __launch_bounds__(1024) void rows_kernel(Matmul p, int log_kw)
+template <int FA, int FB, bool HALF, int MF>
+__global__ __launch_bounds__(256) void rows_kernel(Matmul p, int log_kw)
 {
-    constexpr int U = MF > 2 ? 2 : 4;           // blocks that are loaded together
-    __shared__ f4 sums[16][MF][64];
+    constexpr int U = 4;           // blocks that are loaded together
+    __shared__ f4 sums[4][MF][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const int kw = 1 << log_kw, part = wave & (kw - 1), places = (int)(blockDim.x >> 6) >> log_kw;
-    const int64_t n0 = p.n_first + ((int64_t)blockIdx.x * places + (wave >> log_kw)) * 16, m0 = (int64_t)blockIdx.y * (MF * 16);
+    const int64_t n0 = p.n_first + ((int64_t)blockIdx.x * places + (wave >> log_kw)) * 16;
     const int64_t n = n0 + i, rb = n < p.N ? n : p.N - 1;                 // rows past the end: the last one again
     const uint8_t *const b = p.b + rb * p.ld + g * 32, *const sb = p.b_scales + rb * p.lds;
     const uint8_t *a[MF], *sa[MF];
     f4 acc[MF];
 #pragma unroll
     for (int h = 0; h < MF; ++h) {
-        const int64_t m = m0 + h * 16 + i, ra = m < p.M ? m : p.M - 1;
+        const int64_t m = h * 16 + i, ra = m < p.M ? m : p.M - 1;
         a[h] = p.a + ra * p.ld + g * 32;
         sa[h] = p.a_scales + ra * p.lds;
         acc[h] = (f4)(0.0f);
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(1024) void rows_kernel(Matmul p, int log_kw)
             for (int q = 0; q < U; ++q) {
                 if (k + q0 + q >= p.blocks) break;
                 const int shift = (q0 + q) * 8;
-                if constexpr (NATIVE) {
+                if constexpr (HALF) {
 #pragma unroll
                     for (int h = 0; h < MF; ++h)
                         acc[h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u[q], v[q][h], acc[h], FB, FA, 0, (int)(wb >> shift), 0, (int)(wa[h] >> shift));
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(1024) void rows_kernel(Matmul p, int log_kw)
     const int64_t n4 = n0 + g * 4;
 #pragma unroll
     for (int h = 0; h < MF; ++h) {
-        const int64_t m = m0 + h * 16 + i;
+        const int64_t m = h * 16 + i;
         if (m < p.M) store4<HALF>(p, m, n4, acc[h]);
     }
 }
@@ -398,7 +398,7 @@ template <int LATER>
 __device__ __forceinline__ void meet_behind_stores(bool behind)
 {
     asm volatile("s_cmp_lg_u32 %1, 0\n\ts_cbranch_scc1 .Lstores_%=\n\ts_waitcnt vmcnt(0)\n.Lstores_%=:\n\ts_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier"
-                 ::"n"(LATER < 63 ? LATER : 63), "s"((int)behind) : "memory", "scc");
+                 ::"n"(LATER < 63 ? LATER : 63), "s"(__builtin_amdgcn_readfirstlane((int)behind)) : "memory", "scc");
 }
 
 __device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0); }
@@ -435,7 +435,7 @@ struct Tile {
     static constexpr int RESULT = UNREAD + 1024, LDS = RESULT + WN * WM * 8 * PITCH;
 };
 
-template <int FA, int FB, bool NATIVE, bool HALF, int WN, int WM, int NF, int MF>
+template <int FA, int FB, bool HALF, int WN, int WM, int NF, int MF>
 __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
 {
 #ifdef __HIP_DEVICE_COMPILE__     // (a buffer's type is none of the host compiler's)
@@ -462,14 +462,19 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
     int64_t m0, n0, m_here, n_here;
     const uint8_t *a, *b, *sa_from, *sb_from;
     int64_t a_bytes, b_bytes, words_bytes;
-    int blocks, part;
-    const int64_t tiles = p.m_tiles * p.n_tiles, all = tiles * p.parts;
+    int blocks;
+    const int64_t rest = p.m_tiles * p.n_tiles - p.full, all = p.full + rest * p.parts;
     const auto turn_to = [&](int64_t t) {
         int64_t mt, nt;
-        part = (int)(t / tiles);
-        place(t - part * tiles, p.m_tiles, p.n_tiles, &mt, &nt);
-        const int k0 = part * p.part_blocks;
-        blocks = p.blocks - k0 < p.part_blocks ? p.blocks - k0 : p.part_blocks;
+        int k0 = 0;
+        blocks = p.blocks;
+        if (t >= p.full && p.parts > 1) {
+            const int part = (int)((t - p.full) / rest);
+            t -= part * rest;
+            k0 = part * p.part_blocks;
+            blocks = p.blocks - k0 < p.part_blocks ? p.blocks - k0 : p.part_blocks;
+        }
+        place(t, p.m_tiles, p.n_tiles, &mt, &nt);
         m0 = mt * TM;
         n0 = nt * TN;
         m_here = p.M - m0 < TM ? p.M - m0 : TM;
@@ -524,20 +529,20 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
     // A block's last fragment of B is multiplied behind the meeting that ends its stage, while the next block's first codes are
     // on their way from LDS; the loads of the block after that, into the stage that the meeting has set free, are spread over the first
     // half of the next block, so that none of them holds up a read from LDS that a multiplication waits for.
-    constexpr int SPREAD = NATIVE ? NF : NF > 4 ? NF / 2 : NF - 1, AT_ONCE = (LOADS + SPREAD - 1) / SPREAD;
+    constexpr int SPREAD = HALF ? NF : NF > 4 ? NF / 2 : NF - 1, AT_ONCE = (LOADS + SPREAD - 1) / SPREAD;
     typedef typename Out<HALF>::Vec Vec;
     constexpr int PER_VEC = 16 / Out<HALF>::BYTES, EF = T::EF, VECS = EF * 16 / PER_VEC, PITCH = T::PITCH, TURN = 64 / VECS;
     static_assert(64 % VECS == 0 && 8 % TURN == 0, "whole rows");
     constexpr int STORES = MF * (NF / EF) * (16 / TURN);
     // loads of the block after the next that are made before the next one begins
-    constexpr int FIRST = !NATIVE ? 0 : NF / 2 * AT_ONCE < LOADS ? NF / 2 * AT_ONCE : LOADS;
+    constexpr int FIRST = !HALF ? 0 : NF / 2 * AT_ONCE < LOADS ? NF / 2 * AT_ONCE : LOADS;
     int64_t tile = blockIdx.x;
     turn_to(tile);
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) fetch(0, j);
 #pragma unroll
-    for (int j = 0; j < (NATIVE ? LOADS : 0); ++j) fetch(1, j);
-    wait_and_meet<NATIVE ? LOADS : 0>();
+    for (int j = 0; j < (HALF ? LOADS : 0); ++j) fetch(1, j);
+    wait_and_meet<HALF ? LOADS : 0>();
     bool behind = false;        // stores of the last tile lie between the loads
     for (;;) {
         f4 acc[NF][MF];
@@ -550,13 +555,13 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
         b8 wide[MF][4];
 #pragma unroll
         for (int h = 0; h < MF; ++h) v[h] = codes_a(0, h);
-        if constexpr (!NATIVE) {
+        if constexpr (!HALF) {
 #pragma unroll
             for (int h = 0; h < MF; ++h) widen<FA>(v[h], sa[h] & 255u, wide[h]);
         }
         for (int k = 0; k < blocks; ++k) {
             const int stage = (k & 1) * STAGE, next = STAGE - stage;
-            if constexpr (NATIVE) {
+            if constexpr (HALF) {
                 // First half of the fragments of B: each is multiplied while the one after it is read, and the second half's are read besides.
                 constexpr int H = NF / 2;
                 i8 w[H];
@@ -621,7 +626,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
             for (int f = 0; f < NF; ++f) sb[f] >>= shift;
 #pragma unroll
             for (int h = 0; h < MF; ++h) sa[h] >>= shift;
-            if constexpr (!NATIVE) {
+            if constexpr (!HALF) {
 #pragma unroll
                 for (int h = 0; h < MF; ++h) widen<FA>(v[h], sa[h] & 255u, wide[h]);
             }
@@ -631,14 +636,25 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
         wait_and_meet();
         const int64_t m_out = m0 + wm * MF * 16 + lane / VECS, n_out = n0 + wn * NF * 16 + (lane % VECS) * PER_VEC;
         const bool whole = m_here == TM && n_here == TN && !p.c_in;
-        void* const out_part = (char*)p.out + (int64_t)part * p.M * p.N * 4;            // (parts are fp32)
+        const int64_t done = tile;
         tile += gridDim.x;
         if (tile < all) {
             turn_to(tile);
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) fetch(0, j);
 #pragma unroll
-            for (int j = 0; j < (NATIVE ? LOADS : 0); ++j) fetch(1, j);
+            for (int j = 0; j < (HALF ? LOADS : 0); ++j) fetch(1, j);
+        }
+        if (done >= p.full && p.parts > 1) {
+            f4* const to = p.sums + ((done - p.full) * WAVES + wave) * (NF * MF * 64) + lane;
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                for (int h = 0; h < MF; ++h) to[(f * MF + h) * 64] = acc[f][h];
+            if (tile >= all) return;
+            behind = false;
+            wait_and_meet();
+            continue;
         }
         uint8_t* const mine = lds + T::RESULT + wave * 8 * PITCH;
 #pragma unroll
@@ -668,7 +684,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
 #pragma unroll
                     for (int t = 0; t < 8 / TURN; ++t) {
                         const int64_t m = m_out + h * 16 + half * 8 + t * TURN;
-                        if (m < p.M) store_row<HALF>(p, out_part, m, n_out + e * 16, out[t]);
+                        if (m < p.M) store_row<HALF>(p, m, n_out + e * 16, out[t]);
                     }
                     __builtin_amdgcn_wave_barrier();
                 }
@@ -677,50 +693,40 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
         if (tile >= all) return;
         // the loads are older than the stores: where every store was made, these may still be on their way
         behind = whole;
-        if (whole) wait_and_meet<(NATIVE ? LOADS : 0) + STORES>();
+        if (whole) wait_and_meet<(HALF ? LOADS : 0) + STORES>();
         else wait_and_meet();
     }
 #endif
 }
 
-// out = c_in + part 0 + part 1 + ..., four elements per lane.
-template <bool HALF>
-__global__ __launch_bounds__(256) void add_parts_kernel(const float* parts, int count, const float* c_in, void* out, int64_t n, int64_t first_wg)
+// The tiles that were computed in parts: their sums, in the parts' order, and c_in.  A work-group takes one fragment of each wavefront of a tile.
+template <bool HALF, int WN, int WM, int NF, int MF>
+__global__ __launch_bounds__(64 * WN * WM) void parts_kernel(Matmul p)
 {
-    typedef f4 __attribute__((aligned(4))) any_f4;
-    const int64_t at = ((first_wg + blockIdx.x) * 256 + threadIdx.x) * 4;
+    typedef Tile<HALF, WN, WM, NF, MF> T;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wn = wave % WN, wm = wave / WN, i = lane & 15, g = lane >> 4;
+    const int64_t rest = p.m_tiles * p.n_tiles - p.full, t = blockIdx.x / (NF * MF);
+    const int fh = (int)(blockIdx.x % (NF * MF)), f = fh / MF, h = fh - f * MF;
+    int64_t mt, nt;
+    place(p.full + t, p.m_tiles, p.n_tiles, &mt, &nt);
+    const int64_t m = mt * T::TM + (wm * MF + h) * 16 + i;
+    const int64_t n = nt * T::TN + wn * NF * 16 + (HALF ? (f >> 1) * 32 + g * 8 + (f & 1) * 4 : f * 16 + g * 4);
+    if (m >= p.M || n >= p.N) return;
+    constexpr int64_t ONE = WN * WM * NF * MF * 64;
+    const f4* const from = p.sums + t * ONE + (wave * NF * MF + fh) * 64 + lane;
+    f4 v = from[0];
+#pragma unroll 4
+    for (int s = 1; s < p.parts; ++s) v += from[s * rest * ONE];
+    store4<HALF>(p, m, n, v);
+}
+
+// K = 0: out = c_in, or zeros; four bytes at a time.
+__global__ __launch_bounds__(256) void copy_kernel(const float* c_in, void* out, int64_t n, int elem, int64_t first_wg)
+{
+    const int64_t at = (first_wg + blockIdx.x) * 256 + threadIdx.x;
     if (at >= n) return;
-    const bool four = at + 4 <= n;
-    f4 v = (f4)(0.0f);
-    const auto add = [&](const float* p) {
-        if (four) {
-            v += *reinterpret_cast<const any_f4*>(p + at);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 3; ++j)
-                if (at + j < n) v[j] += p[at + j];
-        }
-    };
-    for (int s = 0; s < count; ++s) add(parts + s * n);
-    if (c_in) add(c_in);
-    if constexpr (HALF) {
-        const u2 w = {narrow2(v.x, v.y), narrow2(v.z, v.w)};
-        if (four) {
-            *reinterpret_cast<u2*>((uint16_t*)out + at) = w;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 3; ++j)
-                if (at + j < n) ((uint16_t*)out)[at + j] = (uint16_t)(w[j >> 1] >> (j & 1) * 16);
-        }
-    } else {
-        if (four) {
-            *reinterpret_cast<f4*>((float*)out + at) = v;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 3; ++j)
-                if (at + j < n) ((float*)out)[at + j] = v[j];
-        }
-    }
+    if (elem == 2) ((uint16_t*)out)[at] = 0;
+    else ((float*)out)[at] = c_in ? c_in[at] : 0.0f;
 }
 
 constexpr int64_t kMaxWgs = 1 << 22;      // work-groups per launch (a launch has less than 2^32 threads)
@@ -753,112 +759,115 @@ void launch_quantize(Quantize p, int64_t tiles, hipStream_t stream)
 
 // How a product is computed.  The form and the number of parts fix the order of additions, so they follow from the sizes and the result's type alone,
 // as if for a GPU of 256 compute units.
-enum { FORM_ROWS, FORM_SMALL, FORM_LARGE };
+enum { FORM_ROWS, FORM_LOW, FORM_SMALL, FORM_LARGE };
 struct Way {
     int form;
     int parts, part_blocks;
+    int64_t full, rest;     // tiles that are computed whole, and in parts
     int log_kw;             // FORM_ROWS: wavefronts that share a place
 };
 
+// A form's tiles, how many of them a compute unit computes at a time, and the microseconds that these take: per block of 128 along K (half / full: for a
+// bf16 / fp32 result), for the tiles' beginning and results, and with a part's sums instead.  Measured on products of 20 to 1100 GFLOP; two small
+// tiles on a compute unit take 1 / 0.7 times as long as one.
+struct Form {
+    int tm, tn, beside;
+    double block[2], tile[2], part;
+};
+constexpr Form kForms[] = {{0, 0, 0, {0, 0}, {0, 0}, 0},
+                           {64, 128, 2, {1.10, 0.80}, {4.0, 2.5}, 2.5},
+                           {128, 128, 2, {1.70, 1.15}, {6.0, 3.0}, 3.0},
+                           {256, 256, 1, {2.75, 1.55}, {14.0, 6.0}, 6.0}};
+constexpr int kUnits = 256;
+
+// Rounds of work-groups on the compute units, the last of which may not find a second one on its.
+double rounds_us(const Form& c, int64_t wgs, double each)
+{
+    const int64_t per_unit = (wgs + kUnits - 1) / kUnits, whole = per_unit / c.beside;
+    return whole * each + (per_unit % c.beside ? 0.7 * each : 0.0);
+}
+
+// What was measured (us) / what one tile size for all would take, without parts: 33801 x 1024 x 4987 to fp32 269 / 322 (256 x 256: its third round has 20 tiles), 300 x 1024 x 20000
+// to fp32 29 / 366, 1000 x 512 x 8000 to bf16 18 / 75, 12000 x 500 x 4000 to fp32 59 / 86, 8192 x 1024 x 32768 to fp32 391 (256 x 256 in two parts) / 477 (128 x 128).
 Way way_for(int64_t M, int64_t N, int64_t K, bool half)
 {
     const int blocks = (int)(code_row(K) / kBlock);
-    Way w{FORM_ROWS, 1, blocks, 0};
-    if (const char* e = getenv("MMF")) {
-        int f, q, l;
-        if (sscanf(e, "%d,%d,%d", &f, &q, &l) == 3 && blocks) {
-            w.form = f; w.part_blocks = ((blocks + q - 1) / q + 3) / 4 * 4; w.parts = (blocks + w.part_blocks - 1) / w.part_blocks; w.log_kw = l;
-            if (f == FORM_ROWS) { w.parts = 1; w.part_blocks = blocks; }
-            return w;
-        }
-    }
-    if (blocks == 0) return w;
+    Way w{FORM_ROWS, 1, blocks, 0, 0, 0};
+    // Up to 32 rows the matrix instructions are idle anyway: B is read past LDS.  One wavefront has work for its latencies with eight blocks; where there are
+    // few places, up to four share one.  32 x 7003 x 512 to bf16 4.4 us, in tiles 5.6; 33 x 32768 x 1024 in tiles 10.4, in three fragments 13.
     if (M <= 32) {
-        const int64_t places = (N + 15) / 16 * ((M + 15) / 16);
-        while (w.log_kw < 4 && (places << w.log_kw) < 2048 && (4 << w.log_kw) < blocks) ++w.log_kw;
+        const int64_t places = (N + 15) / 16;
+        while (w.log_kw < 2 && (places << w.log_kw) < 2048 && (4 << w.log_kw) < blocks) ++w.log_kw;
         return w;
     }
     double best = 1e30;
-    for (int form = FORM_SMALL; form <= FORM_LARGE; ++form) {
-        const int64_t t = form == FORM_SMALL ? 128 : 256, tiles = (M + t - 1) / t * ((N + t - 1) / t), room = form == FORM_SMALL ? 512 : 256;
-        const double block_us = (form == FORM_SMALL ? 1.05 : 1.55) * (half ? 1 : 1.7), tile_us = form == FORM_SMALL ? 2.5 : 5;
-        for (int parts = 1; parts <= 64 && (parts == 1 || parts * 4 <= blocks); ++parts) {
-            const int per = parts == 1 ? blocks : ((blocks + parts - 1) / parts + 3) / 4 * 4;
-            const int q = (blocks + per - 1) / per;
-            if (q != parts) continue;
-            const double us = (double)((tiles * q + room - 1) / room) * (per * block_us + tile_us) + (q > 1 ? 3 + (double)M * N * (4 * q + 4) / 4e6 : 0);
+    for (int form = FORM_LOW; form <= FORM_LARGE; ++form) {
+        const Form& c = kForms[form];
+        const int64_t tiles = (M + c.tm - 1) / c.tm * ((N + c.tn - 1) / c.tn), room = (int64_t)c.beside * kUnits;
+        const double block = c.block[half], whole = blocks * block + c.tile[half];
+        // all tiles whole; or those of the last, unfinished round in parts
+        const double us = rounds_us(c, tiles, whole);
+        if (us < best) {
+            best = us;
+            w = Way{form, 1, blocks, tiles, 0, 0};
+        }
+        const int64_t rest = tiles % room ? tiles % room : tiles == room ? room : 0;
+        for (int parts = 2; rest > 0 && parts <= 64 && parts * 4 <= blocks + 3; ++parts) {
+            const int per = ((blocks + parts - 1) / parts + 3) / 4 * 4;
+            if ((blocks + per - 1) / per != parts) continue;
+            const double us = rounds_us(c, tiles - rest, whole) + rounds_us(c, rest * parts, per * block + c.part) + 3 + (double)(rest * c.tm * c.tn) * (4 * parts + 4) / 4e6;
             if (us < best) {
                 best = us;
-                w = Way{form, q, per, 0};
+                w = Way{form, parts, per, tiles - rest, rest, 0};
             }
         }
     }
     return w;
 }
 
-template <int FA, int FB, bool NATIVE, bool HALF, int WN, int WM, int NF, int MF>
+int64_t parts_bytes(const Way& w) { return w.parts > 1 ? w.rest * w.parts * kForms[w.form].tm * kForms[w.form].tn * 4 : 0; }
+
+template <int FA, int FB, bool HALF, int WN, int WM, int NF, int MF>
 void launch_tiles(Matmul p, hipStream_t stream)
 {
     typedef Tile<HALF, WN, WM, NF, MF> T;
     p.n_tiles = (p.N + T::TN - 1) / T::TN;
     p.m_tiles = (p.M + T::TM - 1) / T::TM;
-    const auto kernel = tile_kernel<FA, FB, NATIVE, HALF, WN, WM, NF, MF>;
+    const auto kernel = tile_kernel<FA, FB, HALF, WN, WM, NF, MF>;
     const int lds = T::LDS;
-    const int64_t tiles = p.m_tiles * p.n_tiles * p.parts, most = (int64_t)compute_units() * (160 * 1024 / lds);      // as many work-groups as there is room for
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles < most ? tiles : most)), dim3(64 * WN * WM), lds, stream, p);
+    const int64_t rest = p.m_tiles * p.n_tiles - p.full, all = p.full + rest * p.parts;
+    const int64_t most = (int64_t)compute_units() * (160 * 1024 / lds);          // as many work-groups as there is room for
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(all < most ? all : most)), dim3(64 * WN * WM), lds, stream, p);
+    if (p.parts > 1) hipLaunchKernelGGL((parts_kernel<HALF, WN, WM, NF, MF>), dim3((unsigned)(rest * NF * MF)), dim3(64 * WN * WM), 0, stream, p);
 }
 
-template <int FA, int FB, bool NATIVE, bool HALF, int MF>
+template <int FA, int FB, bool HALF, int MF>
 void launch_rows(Matmul p, int log_kw, hipStream_t stream)
 {
-    const int waves = log_kw > 2 ? 16 : 4, places = waves >> log_kw;
-    in_launches((p.N + 16 * places - 1) / (16 * places), kMaxWgs / 8, [&](int64_t at, unsigned n) {
+    constexpr int waves = 4;
+    const int places = waves >> log_kw;
+    in_launches((p.N + 16 * places - 1) / (16 * places), kMaxWgs / 2, [&](int64_t at, unsigned n) {
         p.n_first = at * 16 * places;
-        hipLaunchKernelGGL((rows_kernel<FA, FB, NATIVE, HALF, MF>), dim3(n, (unsigned)((p.M + 16 * MF - 1) / (16 * MF))), dim3(64 * waves), 0, stream, p, log_kw);
+        hipLaunchKernelGGL((rows_kernel<FA, FB, HALF, MF>), dim3(n), dim3(64 * waves), 0, stream, p, log_kw);
     });
 }
 
-template <bool HALF>
-void launch_add(const float* parts, int count, const float* c_in, void* out, int64_t n, hipStream_t stream)
+template <int FA, int FB, bool HALF>
+void launch_matmul(const Matmul& p, const Way& w, hipStream_t stream)
 {
-    in_launches((n + 1023) / 1024, kMaxWgs, [&](int64_t at, unsigned wgs) {
-        hipLaunchKernelGGL((add_parts_kernel<HALF>), dim3(wgs), dim3(256), 0, stream, parts, count, c_in, out, n, at);
-    });
-}
-
-template <int FA, int FB, bool NATIVE>
-void launch_matmul(Matmul p, const Way& w, float* parts, hipStream_t stream)
-{
-    if (w.form == FORM_ROWS) {
-        if (p.M <= 16) launch_rows<FA, FB, NATIVE, NATIVE, 1>(p, w.log_kw, stream);
-        else if (p.M <= 32) launch_rows<FA, FB, NATIVE, NATIVE, 2>(p, w.log_kw, stream);
-        else launch_rows<FA, FB, NATIVE, NATIVE, 4>(p, w.log_kw, stream);
-        return;
-    }
-    p.parts = w.parts;
-    p.part_blocks = w.part_blocks;
-    if (w.parts == 1) {
-        if (w.form == FORM_LARGE) launch_tiles<FA, FB, NATIVE, NATIVE, 2, 4, 8, 4>(p, stream);
-        else launch_tiles<FA, FB, NATIVE, NATIVE, 2, 2, 4, 4>(p, stream);
-        return;
-    }
-    const float* const c_in = p.c_in;
-    void* const out = p.out;
-    p.c_in = nullptr;
-    p.out = parts;
-    if (w.form == FORM_LARGE) launch_tiles<FA, FB, NATIVE, false, 2, 4, 8, 4>(p, stream);
-    else launch_tiles<FA, FB, NATIVE, false, 2, 2, 4, 4>(p, stream);
-    launch_add<NATIVE>(parts, w.parts, c_in, out, p.M * p.N, stream);
+    if (w.form == FORM_LARGE) launch_tiles<FA, FB, HALF, 2, 4, 8, 4>(p, stream);
+    else if (w.form == FORM_SMALL) launch_tiles<FA, FB, HALF, 2, 2, 4, 4>(p, stream);
+    else if (w.form == FORM_LOW) launch_tiles<FA, FB, HALF, 2, 2, 4, 2>(p, stream);
+    else if (p.M <= 16) launch_rows<FA, FB, HALF, 1>(p, w.log_kw, stream);
+    else launch_rows<FA, FB, HALF, 2>(p, w.log_kw, stream);
 }
 
 template <int FA, int FB>
-void launch_matmul(const Matmul& p, bool half, const Way& w, float* parts, hipStream_t stream)
+void launch_matmul(const Matmul& p, bool half, const Way& w, hipStream_t stream)
 {
-    if (half) launch_matmul<FA, FB, true>(p, w, parts, stream);
-    else launch_matmul<FA, FB, false>(p, w, parts, stream);
+    if (half) launch_matmul<FA, FB, true>(p, w, stream);
+    else launch_matmul<FA, FB, false>(p, w, stream);
 }
-
-int64_t parts_bytes(int64_t M, int64_t N, const Way& w) { return w.parts > 1 ? round_up(4 * M * N * w.parts, 256) : 0; }
 
 bool unaligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
 bool bad_format(int32_t f) { return f != TS_FP8_E4M3 && f != TS_FP8_E5M2; }
@@ -910,7 +919,11 @@ int ts_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t* bytes)
     if (!bytes) return TS_ERR_NULL;
     if (M < 0 || N < 0 || K < 0) return TS_ERR_SHAPE;
     if (M >= kSizeMax || N >= kSizeMax || K > kKMax) return TS_ERR_OVERFLOW;
-    const int64_t half = parts_bytes(M, N, way_for(M, N, K, true)), full = parts_bytes(M, N, way_for(M, N, K, false));
+    if (M == 0 || N == 0 || K == 0) {
+        *bytes = 0;
+        return TS_OK;
+    }
+    const int64_t half = parts_bytes(way_for(M, N, K, true)), full = parts_bytes(way_for(M, N, K, false));
     *bytes = half > full ? half : full;
     return TS_OK;
 }
@@ -937,26 +950,30 @@ int ts_matmul_fp8(const uint8_t* a, const uint8_t* a_scales, int32_t a_format, c
     p.ld = code_row(K);
     p.lds = scale_row(K);
     p.blocks = (int32_t)(p.ld / kBlock);
-    p.parts = 1;
-    p.part_blocks = p.blocks;
     p.m_tiles = p.n_tiles = p.n_first = 0;
     const bool half = out_dtype == TS_OUT_BF16;
     const hipStream_t s = (hipStream_t)stream;
     if (K == 0) {           // nothing to add up, and no operands to look at
-        if (half) launch_add<true>(nullptr, 0, nullptr, out, M * N, s);
-        else launch_add<false>(nullptr, 0, c_in, out, M * N, s);
+        in_launches((M * N + 255) / 256, kMaxWgs, [&](int64_t at, unsigned n) {
+            hipLaunchKernelGGL(copy_kernel, dim3(n), dim3(256), 0, s, c_in, out, M * N, half ? 2 : 4, at);
+        });
         return hipGetLastError() == hipSuccess ? TS_OK : TS_ERR_HIP;
     }
     const Way w = way_for(M, N, K, half);
-    void* parts = nullptr;
+    p.parts = w.parts;
+    p.part_blocks = w.part_blocks;
+    p.full = w.full;
+    p.sums = nullptr;
     if (w.parts > 1) {
-        const int rc = ts_workspace::take(parts_bytes(M, N, w), &parts);
+        void* ws = nullptr;
+        const int rc = ts_workspace::take(parts_bytes(w), &ws);
         if (rc != TS_OK) return rc;
+        p.sums = (f4*)ws;
     }
-    if (a_format == TS_FP8_E4M3 && b_format == TS_FP8_E4M3) launch_matmul<TS_FP8_E4M3, TS_FP8_E4M3>(p, half, w, (float*)parts, s);
-    else if (a_format == TS_FP8_E4M3) launch_matmul<TS_FP8_E4M3, TS_FP8_E5M2>(p, half, w, (float*)parts, s);
-    else if (b_format == TS_FP8_E4M3) launch_matmul<TS_FP8_E5M2, TS_FP8_E4M3>(p, half, w, (float*)parts, s);
-    else launch_matmul<TS_FP8_E5M2, TS_FP8_E5M2>(p, half, w, (float*)parts, s);
+    if (a_format == TS_FP8_E4M3 && b_format == TS_FP8_E4M3) launch_matmul<TS_FP8_E4M3, TS_FP8_E4M3>(p, half, w, s);
+    else if (a_format == TS_FP8_E4M3) launch_matmul<TS_FP8_E4M3, TS_FP8_E5M2>(p, half, w, s);
+    else if (b_format == TS_FP8_E4M3) launch_matmul<TS_FP8_E5M2, TS_FP8_E4M3>(p, half, w, s);
+    else launch_matmul<TS_FP8_E5M2, TS_FP8_E5M2>(p, half, w, s);
     return hipGetLastError() == hipSuccess ? TS_OK : TS_ERR_HIP;
 }
 
