@@ -435,7 +435,7 @@ struct Tile {
     static constexpr int RESULT = UNREAD + 1024, LDS = RESULT + WN * WM * 8 * PITCH;
 };
 
-template <int FA, int FB, bool HALF, int WN, int WM, int NF, int MF>
+template <int FA, int FB, bool HALF, bool ONTO, int WN, int WM, int NF, int MF>
 __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
 {
 #ifdef __HIP_DEVICE_COMPILE__     // (a buffer's type is none of the host compiler's)
@@ -533,6 +533,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
     typedef typename Out<HALF>::Vec Vec;
     constexpr int PER_VEC = 16 / Out<HALF>::BYTES, EF = T::EF, VECS = EF * 16 / PER_VEC, PITCH = T::PITCH, TURN = 64 / VECS;
     static_assert(64 % VECS == 0 && 8 % TURN == 0, "whole rows");
+    constexpr int NT = 2;           // nontemporal
     constexpr int STORES = MF * (NF / EF) * (16 / TURN);
     // loads of the block after the next that are made before the next one begins
     constexpr int FIRST = !HALF ? 0 : NF / 2 * AT_ONCE < LOADS ? NF / 2 * AT_ONCE : LOADS;
@@ -635,8 +636,14 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
         // stretches of 256 bytes; each has a place of its own, and waits for nobody.
         wait_and_meet();
         const int64_t m_out = m0 + wm * MF * 16 + lane / VECS, n_out = n0 + wn * NF * 16 + (lane % VECS) * PER_VEC;
-        const bool whole = m_here == TM && n_here == TN && !p.c_in;
+        const bool whole_tile = m_here == TM && n_here == TN, whole = whole_tile && !ONTO;
         const int64_t done = tile;
+        const bool in_parts = done >= p.full && p.parts > 1;
+        // c_in of a whole tile is asked for sixteen rows at a time (asked for where it is added, every store waited for it: 33801 x 1024 x 4987 onto fp32
+        // 331 us, so 305), by way of a buffer, whose addresses are one register for all rows.
+        const bool ahead = ONTO && whole_tile && p.N <= 1 << 20;
+        const int64_t corner = (m0 + wm * MF * 16) * p.N + n0 + wn * NF * 16;
+        const uint32_t row_bytes = (uint32_t)p.N * 4, from_corner = (uint32_t)(lane / VECS) * row_bytes + (uint32_t)(lane % VECS) * 16;
         tile += gridDim.x;
         if (tile < all) {
             turn_to(tile);
@@ -645,7 +652,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
 #pragma unroll
             for (int j = 0; j < (HALF ? LOADS : 0); ++j) fetch(1, j);
         }
-        if (done >= p.full && p.parts > 1) {
+        if (in_parts) {
             f4* const to = p.sums + ((done - p.full) * WAVES + wave) * (NF * MF * 64) + lane;
 #pragma unroll
             for (int f = 0; f < NF; ++f)
@@ -659,6 +666,16 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
         uint8_t* const mine = lds + T::RESULT + wave * 8 * PITCH;
 #pragma unroll
         for (int h = 0; h < MF; ++h) {
+            f4 c[NF / EF][16 / TURN];
+            if (ahead) {
+                const __amdgpu_buffer_rsrc_t onto = buffer((const uint8_t*)(p.c_in + corner), 0x7FFFFFFF);
+                keep_order();
+#pragma unroll
+                for (int e = 0; e < NF; e += EF)
+#pragma unroll
+                    for (int t = 0; t < 16 / TURN; ++t)
+                        c[e / EF][t] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(onto, from_corner, (h * 16 + t * TURN) * row_bytes + e * 64, NT));
+            }
 #pragma unroll
             for (int e = 0; e < NF; e += EF) {
 #pragma unroll
@@ -684,7 +701,14 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
 #pragma unroll
                     for (int t = 0; t < 8 / TURN; ++t) {
                         const int64_t m = m_out + h * 16 + half * 8 + t * TURN;
-                        if (m < p.M) store_row<HALF>(p, m, n_out + e * 16, out[t]);
+                        if (ahead) {
+                            if constexpr (!HALF)
+                                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, out[t] + c[e / EF][half * (8 / TURN) + t]),
+                                                                       buffer((const uint8_t*)((const float*)p.out + corner), 0x7FFFFFFF), from_corner,
+                                                                       (h * 16 + half * 8 + t * TURN) * row_bytes + e * 64, NT);
+                        } else if (m < p.M) {
+                            store_row<HALF>(p, m, n_out + e * 16, out[t]);
+                        }
                     }
                     __builtin_amdgcn_wave_barrier();
                 }
@@ -833,7 +857,7 @@ void launch_tiles(Matmul p, hipStream_t stream)
     typedef Tile<HALF, WN, WM, NF, MF> T;
     p.n_tiles = (p.N + T::TN - 1) / T::TN;
     p.m_tiles = (p.M + T::TM - 1) / T::TM;
-    const auto kernel = tile_kernel<FA, FB, HALF, WN, WM, NF, MF>;
+    const auto kernel = !HALF && p.c_in ? tile_kernel<FA, FB, HALF, !HALF, WN, WM, NF, MF> : tile_kernel<FA, FB, HALF, false, WN, WM, NF, MF>;
     const int lds = T::LDS;
     const int64_t rest = p.m_tiles * p.n_tiles - p.full, all = p.full + rest * p.parts;
     const int64_t most = (int64_t)compute_units() * (160 * 1024 / lds);          // as many work-groups as there is room for
