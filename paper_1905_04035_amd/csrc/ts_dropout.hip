@@ -30,6 +30,10 @@ __device__ __forceinline__ f4 widen4(u2 b)
 }
 __device__ __forceinline__ f4 load4(const uint16_t* p) { return widen4(__builtin_nontemporal_load(reinterpret_cast<const u2*>(p))); }
 
+// The same for rows that are read again: those of hot ids, and of positions.
+__device__ __forceinline__ f4 load4_kept(const float* p) { return *reinterpret_cast<const f4*>(p); }
+__device__ __forceinline__ f4 load4_kept(const uint16_t* p) { return widen4(*reinterpret_cast<const u2*>(p)); }
+
 // bf16, nearest with ties to even: one instruction for two elements.
 __device__ __forceinline__ uint32_t narrow2(float x, float y)
 {
@@ -66,22 +70,34 @@ struct Lookup {
 };
 
 // out[t] = dropout(scale * weight[ids[t]] + pos[pos_ids[t]]).  A row belongs to `lanes` neighbouring lanes (a power of two), a
-// work-group takes 4 * 64 / lanes rows and, where rows are wider than 64 lanes, one block of 256 of their columns.
-template <typename W, typename O>
+// work-group takes 4 * 64 / lanes rows and, where rows are wider than 64 lanes, one block of CH * 256 of their columns.
+template <typename W, typename O, int CH>
 __global__ __launch_bounds__(kThreads) void lookup_kernel(Lookup p, int log_lanes)
 {
     const int64_t t = p.row_first + ((int64_t)blockIdx.x * (kThreads >> log_lanes) + (threadIdx.x >> log_lanes));
-    const int col = ((int)blockIdx.y * 64 + (int)(threadIdx.x & ((1u << log_lanes) - 1u))) * 4;
-    if (t >= p.n || col >= p.d) return;
+    const int col0 = ((int)blockIdx.y * (64 * CH) + (int)(threadIdx.x & ((1u << log_lanes) - 1u))) * 4;
+    if (t >= p.n || col0 >= p.d) return;
     const int32_t id = p.ids[t];
     const int32_t at = p.pos ? p.pos_ids[t] : -1;
-    f4 v = (f4)(0.0f), q = (f4)(0.0f);
-    if ((uint32_t)id < (uint32_t)p.V) v = load4((const W*)p.weight + (size_t)id * p.d + col);
-    if ((uint32_t)at < (uint32_t)p.n_pos) q = load4((const W*)p.pos + (size_t)at * p.d + col);
+    const bool has_row = (uint32_t)id < (uint32_t)p.V, has_pos = (uint32_t)at < (uint32_t)p.n_pos;
+    f4 v[CH], q[CH];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = fmaf(v[i], p.scale, q[i]);
-    const int64_t e = t * p.d + col;
-    store4((O*)p.out + e, ts_mask::apply<false>(v, (f4)(0.0f), (uint64_t)e >> 2, ts_mask::offset_now(p.m), p.m));
+    for (int c = 0; c < CH; ++c) {
+        const int col = col0 + c * 256;
+        v[c] = q[c] = (f4)(0.0f);
+        if (has_row && col < p.d) v[c] = load4_kept((const W*)p.weight + (size_t)id * p.d + col);
+        if (has_pos && col < p.d) q[c] = load4_kept((const W*)p.pos + (size_t)at * p.d + col);
+    }
+    const uint64_t offset = ts_mask::offset_now(p.m);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = col0 + c * 256;
+        if (col >= p.d) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[c][i] = fmaf(v[c][i], p.scale, q[c][i]);
+        const int64_t e = t * p.d + col;
+        store4((O*)p.out + e, ts_mask::apply<false>(v[c], (f4)(0.0f), (uint64_t)e >> 2, offset, p.m));
+    }
 }
 
 template <typename T>
@@ -104,13 +120,15 @@ void launch_lookup(Lookup p, hipStream_t stream)
     int log_lanes = 0;
     while (log_lanes < 6 && (4 << log_lanes) < p.d) ++log_lanes;
     const int rows = kThreads >> log_lanes;
-    const unsigned blocks = (unsigned)((p.d + 255) / 256);
+    const bool wide = p.d > 256;
+    const unsigned blocks = (unsigned)(wide ? (p.d + 1023) / 1024 : 1);
     const int64_t most = kMaxWgs / blocks > 0 ? kMaxWgs / blocks : 1;
     for (int64_t at = 0; at < p.n;) {
         const int64_t wgs = (p.n - at + rows - 1) / rows;
         const dim3 grid((unsigned)(wgs < most ? wgs : most), blocks);
         p.row_first = at;
-        hipLaunchKernelGGL((lookup_kernel<W, O>), grid, dim3(kThreads), 0, stream, p, log_lanes);
+        if (wide) hipLaunchKernelGGL((lookup_kernel<W, O, 4>), grid, dim3(kThreads), 0, stream, p, log_lanes);
+        else hipLaunchKernelGGL((lookup_kernel<W, O, 1>), grid, dim3(kThreads), 0, stream, p, log_lanes);
         at += (int64_t)grid.x * rows;
     }
 }

@@ -41,21 +41,50 @@ __device__ __forceinline__ uint32_t narrow2(float x, float y)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
 }
 
+// The t-th tile.  Work-groups b, b + 8, b + 16, ... run on one of eight XCDs with an L2 each: every XCD takes neighbouring tiles, kStrip of them along
+// M before the next along N, so that those it works on at one time share their operands, and write long stretches of the result's rows.
+// 8192 x 32768 x 1024 to bf16 with strips of 1 / 2 / 4 / 8 / 16: 310 / 299 / 290 / 325 / 327 us, 8192^3 487 / 459 / 460 / 469 / 470.
+template <int kStrip = 4>
+__device__ __forceinline__ void place(int64_t wg, int64_t m_tiles, int64_t n_tiles, int64_t* mt, int64_t* nt)
+{
+    const int64_t tiles = m_tiles * n_tiles, each = tiles >> 3, rest = tiles & 7, x = wg & 7;
+    const int64_t t = x * each + (x < rest ? x : rest) + (wg >> 3);
+    const int64_t strip = kStrip * n_tiles, s = t / strip, at = t - s * strip;
+    const int64_t high = m_tiles - s * kStrip < kStrip ? m_tiles - s * kStrip : kStrip;
+    *nt = at / high;
+    *mt = s * kStrip + (at - *nt * high);
+}
+
 // ------------------------------------------------------------------ codes and scales
-// Byte of the scale of a block whose largest finite magnitude is `most`: e + 127 for the smallest e >= -127 with
+// Byte of the scale of a block whose largest finite magnitude has these bits: e + 127 for the smallest e >= -127 with
 // most <= MAX 2^e, where MAX is 1.75 * 2^8 (e4m3) or 1.75 * 2^15 (e5m2).
 template <int FMT>
-__device__ __forceinline__ uint32_t scale_byte(float most)
+__device__ __forceinline__ uint32_t scale_byte(uint32_t most)
 {
-    const uint32_t b = __float_as_uint(most);
-    const int e = (int)(b >> 23) - (FMT == TS_FP8_E4M3 ? 8 : 15) + ((b & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    const int e = (int)(most >> 23) - (FMT == TS_FP8_E4M3 ? 8 : 15) + ((most & 0x7FFFFFu) > 0x600000u ? 1 : 0);
     return (uint32_t)(e < 0 ? 0 : e);
 }
 
-__device__ __forceinline__ float finite_size(float x)
+constexpr uint32_t kInfinite = 0x7F800000u;          // bits of magnitudes: infinities and NaN lie above all numbers
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// The largest of sixteen neighbouring lanes, by rotations within them.
+template <int N>
+__device__ __forceinline__ uint32_t rotated(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x120 + N, 0xf, 0xf, true); }
+__device__ __forceinline__ uint32_t largest_of_16(uint32_t x)
 {
-    const float a = fabsf(x);
-    return a < __builtin_inff() ? a : 0.0f;
+    x = larger(x, rotated<8>(x));
+    x = larger(x, rotated<4>(x));
+    x = larger(x, rotated<2>(x));
+    return larger(x, rotated<1>(x));
+}
+// The largest of lanes i, i + 16, i + 32 and i + 48.
+__device__ __forceinline__ uint32_t largest_of_rows(uint32_t x)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = larger(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return larger(b[0], b[1]);
 }
 
 // Four codes of x * 2^(127 - byte).  (byte <= 247, so the factor is a normal number.)
@@ -79,70 +108,150 @@ struct Quantize {
     uint8_t *q, *q_scales, *qt, *qt_scales;
     int64_t rows, cols;
     int64_t tile_first;
-    int64_t col_tiles;
+    int64_t row_tiles, col_tiles;
 };
 
-__device__ __forceinline__ float widen1(const float* p) { return *p; }
-__device__ __forceinline__ float widen1(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
-__device__ __forceinline__ f4 widen4(const float* p) { return *reinterpret_cast<const f4*>(p); }
-__device__ __forceinline__ f4 widen4(const uint16_t* p)
-{
-    const u2 b = *reinterpret_cast<const u2*>(p);
-    f4 r;
-    r.x = __uint_as_float(b.x << 16);
-    r.y = __uint_as_float(b.x & 0xFFFF0000u);
-    r.z = __uint_as_float(b.y << 16);
-    r.w = __uint_as_float(b.y & 0xFFFF0000u);
-    return r;
-}
+// Eight rows of eight elements as they lie in memory, zeros beyond the matrix; and the bits of the largest magnitudes of a row and of all columns,
+// which show whether a value is no finite number.
+template <typename T>
+struct Part;
 
-// A work-group takes a tile of 128 x 128 elements, a thread 8 x 8 of them.  A row's block is in the registers of sixteen
-// neighbouring lanes; a column's in those of every sixteenth thread.
-template <typename T, int FMT, bool VEC>
-__global__ __launch_bounds__(256) void quantize_kernel(Quantize p)
-{
-    __shared__ float most_of[4][kBlock];
-    __shared__ __align__(16) uint8_t turned[kBlock][kBlock + 16];
-    const int64_t tile = p.tile_first + blockIdx.x;
-    const int64_t r_tile = tile / p.col_tiles, c_tile = tile - r_tile * p.col_tiles;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const int r8 = (tid >> 4) * 8, c8 = (tid & 15) * 8;       // the thread's place in the tile
-    const int64_t r0 = r_tile * kBlock + r8, c0 = c_tile * kBlock + c8;
+template <>
+struct Part<float> {
     f4 v[8][2];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const T* const row = (const T*)p.x + (r0 + i) * p.cols + c0;
+
+    template <int VEC>
+    __device__ __forceinline__ void load(int i, const float* p, int64_t left)
+    {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             v[i][h] = (f4)(0.0f);
-            if (r0 + i < p.rows) {
-                if (VEC) {
-                    if (c0 + 4 * h < p.cols) v[i][h] = widen4(row + 4 * h);
-                } else {
+            if (VEC >= 4) {
+                if (4 * h < left) v[i][h] = __builtin_nontemporal_load(reinterpret_cast<const f4*>(p) + h);
+            } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (c0 + 4 * h + j < p.cols) v[i][h][j] = widen1(row + 4 * h + j);
-                }
+                for (int j = 0; j < 4; ++j)
+                    if (4 * h + j < left) v[i][h][j] = p[4 * h + j];
             }
         }
     }
+    __device__ __forceinline__ float value(int i, int c) const { return v[i][c >> 2][c & 3]; }
+    __device__ __forceinline__ f4 four(int i, int h) const { return v[i][h]; }
+    // (two magnitudes in one instruction; a quiet NaN is passed over, as it should be)
+    static __device__ __forceinline__ float larger3(float most, float a, float b)
+    {
+        asm("v_max3_f32 %0, |%1|, |%2|, %3" : "=v"(most) : "v"(a), "v"(b), "v"(most));
+        return most;
+    }
+    __device__ __forceinline__ uint32_t row_size(int i) const
+    {
+        float m = 0.0f;
+#pragma unroll
+        for (int c = 0; c < 8; c += 2) m = larger3(m, value(i, c), value(i, c + 1));
+        return __float_as_uint(m) & 0x7FFFFFFFu;
+    }
+    __device__ __forceinline__ void column_sizes(uint32_t (&most)[8]) const
+    {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            float m = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) m = larger3(m, value(i, c), value(i + 1, c));
+            most[c] = __float_as_uint(m) & 0x7FFFFFFFu;
+        }
+    }
+};
+
+template <>
+struct Part<uint16_t> {
+    typedef uint16_t h2 __attribute__((ext_vector_type(2)));
+    u4 v[8];
+
+    template <int VEC>
+    __device__ __forceinline__ void load(int i, const uint16_t* p, int64_t left)
+    {
+        v[i] = (u4)(0u);
+        if (VEC == 8) {
+            if (left > 0) v[i] = __builtin_nontemporal_load(reinterpret_cast<const u4*>(p));
+        } else if (VEC == 4) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (4 * h < left) {
+                    const u2 w = __builtin_nontemporal_load(reinterpret_cast<const u2*>(p) + h);
+                    v[i][2 * h] = w.x;
+                    v[i][2 * h + 1] = w.y;
+                }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < left) v[i][j >> 1] |= (uint32_t)p[j] << (j & 1) * 16;
+        }
+    }
+    __device__ __forceinline__ float value(int i, int c) const { return __uint_as_float(c & 1 ? v[i][c >> 1] & 0xFFFF0000u : v[i][c >> 1] << 16); }
+    __device__ __forceinline__ f4 four(int i, int h) const { return f4{value(i, 4 * h), value(i, 4 * h + 1), value(i, 4 * h + 2), value(i, 4 * h + 3)}; }
+    // (two magnitudes in one instruction, as 16-bit numbers)
+    static __device__ __forceinline__ uint32_t larger2(uint32_t most, uint32_t w)
+    {
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(h2, most), __builtin_bit_cast(h2, w & 0x7FFF7FFFu)));
+    }
+    __device__ __forceinline__ uint32_t row_size(int i) const
+    {
+        uint32_t m = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) m = larger2(m, v[i][k]);
+        return larger(m << 16, m & 0xFFFF0000u);
+    }
+    __device__ __forceinline__ void column_sizes(uint32_t (&most)[8]) const
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = larger2(m, v[i][k]);
+            most[2 * k] = m << 16;
+            most[2 * k + 1] = m & 0xFFFF0000u;
+        }
+    }
+};
+
+__device__ __forceinline__ uint32_t finite_size(float x)
+{
+    const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
+    return b < kInfinite ? b : 0u;
+}
+
+// A work-group takes a tile of 128 x 128 elements, a thread 8 x 8 of them.  A row's block is in the registers of sixteen
+// neighbouring lanes; a column's in those of every sixteenth thread.  Where a largest magnitude is that of an infinity or NaN, the elements are
+// looked at again without them.  Bound by memory, and so by how many tiles a compute unit holds: bf16 elements stay as they are, two to a register.
+// 8192 x 32768 bf16 to e5m2, both ways / rows only: XXX.
+template <typename T, int FMT, int VEC>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 5 : 4) void quantize_kernel(Quantize p)
+{
+    __shared__ __align__(16) uint32_t most_of[4][kBlock];
+    __shared__ __align__(16) uint8_t turned[kBlock][kBlock + 16];
+    int64_t r_tile, c_tile;
+    place<3>(p.tile_first + blockIdx.x, p.row_tiles, p.col_tiles, &r_tile, &c_tile);
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int r8 = (tid >> 4) * 8, c8 = (tid & 15) * 8;       // the thread's place in the tile
+    const int64_t r0 = r_tile * kBlock + r8, c0 = c_tile * kBlock + c8;
+    Part<T> x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x.template load<VEC>(i, (const T*)p.x + (r0 + i) * p.cols + c0, r0 + i < p.rows ? p.cols - c0 : 0);
     if (p.q) {
         const int64_t ld = code_row(p.cols), lds = scale_row(p.cols);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            float most = 0.0f;
+            uint32_t most = largest_of_16(x.row_size(i));
+            if (__any(most >= kInfinite)) {
+                most = 0;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) most = fmaxf(most, finite_size(v[i][h][j]));
-#pragma unroll
-            for (int m = 1; m < 16; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+                for (int c = 0; c < 8; ++c) most = larger(most, finite_size(x.value(i, c)));
+                most = largest_of_16(most);
+            }
             const uint32_t byte = scale_byte<FMT>(most);
             if (r0 + i < p.rows) {
-                u2 w;
-                w.x = codes4<FMT>(v[i][0], byte);
-                w.y = codes4<FMT>(v[i][1], byte);
-                *reinterpret_cast<u2*>(p.q + (r0 + i) * ld + c0) = w;
+                const u2 w = {codes4<FMT>(x.four(i, 0), byte), codes4<FMT>(x.four(i, 1), byte)};
+                __builtin_nontemporal_store(w, reinterpret_cast<u2*>(p.q + (r0 + i) * ld + c0));
                 // lane 0 of the sixteen writes the block's byte; behind the last block, lanes 1 to 3 the zeros
                 const int64_t at = c_tile + (lane & 15);
                 if ((lane & 15) == 0) p.q_scales[(r0 + i) * lds + at] = (uint8_t)byte;
@@ -151,49 +260,59 @@ __global__ __launch_bounds__(256) void quantize_kernel(Quantize p)
         }
     }
     if (!p.qt) return;
-    f4 most[2] = {(f4)(0.0f), (f4)(0.0f)};
+    uint32_t most[8];
+    x.column_sizes(most);
+    uint32_t all = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int c = 0; c < 8; ++c) {
+        most[c] = largest_of_rows(most[c]);
+        all = larger(all, most[c]);
+    }
+    if (__any(all >= kInfinite)) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int c = 0; c < 8; ++c) {
+            most[c] = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) most[h][j] = fmaxf(most[h][j], finite_size(v[i][h][j]));
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            most[h][j] = fmaxf(most[h][j], __shfl_xor(most[h][j], 16));
-            most[h][j] = fmaxf(most[h][j], __shfl_xor(most[h][j], 32));
-            if (lane < 16) most_of[wave][c8 + 4 * h + j] = most[h][j];
+            for (int i = 0; i < 8; ++i) most[c] = larger(most[c], finite_size(x.value(i, c)));
+            most[c] = largest_of_rows(most[c]);
         }
-    __syncthreads();
-    const int64_t ld = code_row(p.rows), lds = scale_row(p.rows), row_tiles = (p.rows + kBlock - 1) / kBlock;
+    }
+    if (lane < 16) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) *reinterpret_cast<u4*>(&most_of[wave][c8 + 4 * h]) = u4{most[4 * h], most[4 * h + 1], most[4 * h + 2], most[4 * h + 3]};
+    }
+    __syncthreads();
+    const int64_t ld = code_row(p.rows), lds = scale_row(p.rows);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        u4 m = (u4)(0u);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const u4 a = *reinterpret_cast<const u4*>(&most_of[w][c8 + 4 * h]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) m[j] = larger(m[j], a[j]);
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int c = c8 + 4 * h + j;
-            const float m = fmaxf(fmaxf(most_of[0][c], most_of[1][c]), fmaxf(most_of[2][c], most_of[3][c]));
-            const uint32_t byte = scale_byte<FMT>(m);
-            const f4 lo = {v[0][h][j], v[1][h][j], v[2][h][j], v[3][h][j]}, hi = {v[4][h][j], v[5][h][j], v[6][h][j], v[7][h][j]};
-            u2 w;
-            w.x = codes4<FMT>(lo, byte);
-            w.y = codes4<FMT>(hi, byte);
-            *reinterpret_cast<u2*>(&turned[c][r8]) = w;
-            if (r8 == 0 && c0 + 4 * h + j < p.cols) {
-                uint8_t* const s = p.qt_scales + (c0 + 4 * h + j) * lds;
+            const int c = 4 * h + j;
+            const uint32_t byte = scale_byte<FMT>(m[j]);
+            const f4 lo = {x.value(0, c), x.value(1, c), x.value(2, c), x.value(3, c)}, hi = {x.value(4, c), x.value(5, c), x.value(6, c), x.value(7, c)};
+            *reinterpret_cast<u2*>(&turned[c8 + c][r8]) = u2{codes4<FMT>(lo, byte), codes4<FMT>(hi, byte)};
+            if (r8 == 0 && c0 + c < p.cols) {
+                uint8_t* const s = p.qt_scales + (c0 + c) * lds;
                 s[r_tile] = (uint8_t)byte;
-                if (r_tile == row_tiles - 1)
-                    for (int64_t at = row_tiles; at < lds; ++at) s[at] = 0;
+                if (r_tile == p.row_tiles - 1)
+                    for (int64_t at = p.row_tiles; at < lds; ++at) s[at] = 0;
             }
         }
+    }
     __syncthreads();
     // eight lanes to a row of 128 codes
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int c = i * 32 + (tid >> 3), at = (tid & 7) * 16;
         if (c_tile * kBlock + c < p.cols)
-            *reinterpret_cast<u4*>(p.qt + (c_tile * kBlock + c) * ld + r_tile * kBlock + at) = *reinterpret_cast<const u4*>(&turned[c][at]);
+            __builtin_nontemporal_store(*reinterpret_cast<const u4*>(&turned[c][at]), reinterpret_cast<u4*>(p.qt + (c_tile * kBlock + c) * ld + r_tile * kBlock + at));
     }
 }
 
@@ -410,21 +529,6 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const uint8_t* p, int64
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, (int)(uint32_t)(bytes < 0xFFFFFFFFll ? bytes : 0xFFFFFFFFll), 0x00020000);
 }
 #endif
-
-// The t-th tile.  Work-groups b, b + 8, b + 16, ... run on one of eight XCDs with an L2 each: every XCD takes neighbouring tiles, kStrip of them along
-// M before the next along N, so that those it works on at one time share their operands, and write long stretches of the result's rows.
-// 8192 x 32768 x 1024 to bf16 with strips of 1 / 2 / 4 / 8 / 16: 310 / 299 / 290 / 325 / 327 us, 8192^3 487 / 459 / 460 / 469 / 470.
-constexpr int kStrip = 4;
-
-__device__ __forceinline__ void place(int64_t wg, int64_t m_tiles, int64_t n_tiles, int64_t* mt, int64_t* nt)
-{
-    const int64_t tiles = m_tiles * n_tiles, each = tiles >> 3, rest = tiles & 7, x = wg & 7;
-    const int64_t t = x * each + (x < rest ? x : rest) + (wg >> 3);
-    const int64_t strip = kStrip * n_tiles, s = t / strip, at = t - s * strip;
-    const int64_t high = m_tiles - s * kStrip < kStrip ? m_tiles - s * kStrip : kStrip;
-    *nt = at / high;
-    *mt = s * kStrip + (at - *nt * high);
-}
 
 // Sizes that the host needs, too.  LDS: two stages of [ROWS][128] codes, two of [ROWS] words of scales, 1 KiB that nobody reads, and eight rows of
 // the result for every wavefront.
@@ -776,8 +880,9 @@ void launch_quantize(Quantize p, int64_t tiles, hipStream_t stream)
 {
     in_launches(tiles, kMaxWgs, [&](int64_t at, unsigned n) {
         p.tile_first = at;
-        if (p.cols % 4 == 0) hipLaunchKernelGGL((quantize_kernel<T, FMT, true>), dim3(n), dim3(256), 0, stream, p);
-        else hipLaunchKernelGGL((quantize_kernel<T, FMT, false>), dim3(n), dim3(256), 0, stream, p);
+        if (p.cols % 8 == 0) hipLaunchKernelGGL((quantize_kernel<T, FMT, 8>), dim3(n), dim3(256), 0, stream, p);
+        else if (p.cols % 4 == 0) hipLaunchKernelGGL((quantize_kernel<T, FMT, 4>), dim3(n), dim3(256), 0, stream, p);
+        else hipLaunchKernelGGL((quantize_kernel<T, FMT, 1>), dim3(n), dim3(256), 0, stream, p);
     });
 }
 
@@ -928,8 +1033,9 @@ int ts_quantize_fp8(const void* x, int32_t x_dtype, int64_t rows, int64_t cols, 
     p.qt_scales = qt_scales;
     p.rows = rows;
     p.cols = cols;
+    p.row_tiles = (rows + kBlock - 1) / kBlock;
     p.col_tiles = (cols + kBlock - 1) / kBlock;
-    const int64_t tiles = (rows + kBlock - 1) / kBlock * p.col_tiles;
+    const int64_t tiles = p.row_tiles * p.col_tiles;
     const hipStream_t s = (hipStream_t)stream;
     if (x_dtype == TS_ROW_BF16 && format == TS_FP8_E4M3) launch_quantize<uint16_t, TS_FP8_E4M3>(p, tiles, s);
     else if (x_dtype == TS_ROW_BF16) launch_quantize<uint16_t, TS_FP8_E5M2>(p, tiles, s);
