@@ -245,7 +245,7 @@ int ts_quantize_fp8(const void* x, int32_t x_dtype, int64_t rows, int64_t cols, 
  * product has more than 13 bits below the largest of its group of eight along K (1.5e-5 of the result's norm on normal
  * data), and rounded once; c_in must be NULL with TS_OUT_BF16, else TS_ERR_SHAPE.  c_in fp32 [M, N] or NULL; it may be
  * out.  M, N or K may be 0 (K = 0: out = c_in or zeros).  a, b: 16-byte aligned, scales: 4-byte, out and c_in: 16-byte.  M, N
- * below 2^31, K at most 2^24.
+ * below 2^31, K at most 2^24 - 128.
  * A product of few rows and columns is split along K and uses the bound workspace, ts_matmul_workspace_bytes(M, N, K)
  * bytes of it (0 where it is not split); what ts_last_views described in that workspace is then gone.
  */

@@ -15,6 +15,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "ts_densify.h"
 #include "ts_workspace.h"
 
@@ -41,18 +43,19 @@ __device__ __forceinline__ uint32_t narrow2(float x, float y)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
 }
 
-// The t-th tile.  Work-groups b, b + 8, b + 16, ... run on one of eight XCDs with an L2 each: every XCD takes neighbouring tiles, kStrip of them along
+// The t-th tile.  Work-groups b, b + 8, b + 16, ... run on one of eight XCDs with an L2 each: every XCD takes neighbouring tiles, STRIP of them along
 // M before the next along N, so that those it works on at one time share their operands, and write long stretches of the result's rows.
+// (Codes and scales are made in strips of 3: 2-3 % before 2 and 4, whose rows' addresses fall on fewer memory channels.)
 // 8192 x 32768 x 1024 to bf16 with strips of 1 / 2 / 4 / 8 / 16: 310 / 299 / 290 / 325 / 327 us, 8192^3 487 / 459 / 460 / 469 / 470.
-template <int kStrip = 4>
+template <int STRIP = 4>
 __device__ __forceinline__ void place(int64_t wg, int64_t m_tiles, int64_t n_tiles, int64_t* mt, int64_t* nt)
 {
     const int64_t tiles = m_tiles * n_tiles, each = tiles >> 3, rest = tiles & 7, x = wg & 7;
     const int64_t t = x * each + (x < rest ? x : rest) + (wg >> 3);
-    const int64_t strip = kStrip * n_tiles, s = t / strip, at = t - s * strip;
-    const int64_t high = m_tiles - s * kStrip < kStrip ? m_tiles - s * kStrip : kStrip;
+    const int64_t strip = STRIP * n_tiles, s = t / strip, at = t - s * strip;
+    const int64_t high = m_tiles - s * STRIP < STRIP ? m_tiles - s * STRIP : STRIP;
     *nt = at / high;
-    *mt = s * kStrip + (at - *nt * high);
+    *mt = s * STRIP + (at - *nt * high);
 }
 
 // ------------------------------------------------------------------ codes and scales
@@ -223,12 +226,12 @@ __device__ __forceinline__ uint32_t finite_size(float x)
 // A work-group takes a tile of 128 x 128 elements, a thread 8 x 8 of them.  A row's block is in the registers of sixteen
 // neighbouring lanes; a column's in those of every sixteenth thread.  Where a largest magnitude is that of an infinity or NaN, the elements are
 // looked at again without them.  Bound by memory, and so by how many tiles a compute unit holds: bf16 elements stay as they are, two to a register.
-// 8192 x 32768 bf16 to e5m2, both ways / rows only: XXX.
+// 8192 x 32768 bf16 to e5m2, both ways / rows only: 208 us = 5.2 TB/s / 145 = 5.6 (261 / 181 with fp32 in the registers and every magnitude by itself).
 template <typename T, int FMT, int VEC>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 5 : 4) void quantize_kernel(Quantize p)
 {
     __shared__ __align__(16) uint32_t most_of[4][kBlock];
-    __shared__ __align__(16) uint8_t turned[kBlock][kBlock + 16];
+    __shared__ __align__(16) uint8_t turned[kBlock][kBlock + 8];
     int64_t r_tile, c_tile;
     place<3>(p.tile_first + blockIdx.x, p.row_tiles, p.col_tiles, &r_tile, &c_tile);
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -312,7 +315,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 5 : 4) void quantize_kernel(Q
     for (int i = 0; i < 4; ++i) {
         const int c = i * 32 + (tid >> 3), at = (tid & 7) * 16;
         if (c_tile * kBlock + c < p.cols)
-            __builtin_nontemporal_store(*reinterpret_cast<const u4*>(&turned[c][at]), reinterpret_cast<u4*>(p.qt + (c_tile * kBlock + c) * ld + r_tile * kBlock + at));
+            __builtin_nontemporal_store(__builtin_shufflevector(*reinterpret_cast<const u2*>(&turned[c][at]), *reinterpret_cast<const u2*>(&turned[c][at + 8]), 0, 1, 2, 3), reinterpret_cast<u4*>(p.qt + (c_tile * kBlock + c) * ld + r_tile * kBlock + at));
     }
 }
 
@@ -356,25 +359,23 @@ __device__ __forceinline__ void widen(i8 codes, uint32_t scale, b8 (&out)[4])
 }
 
 // 16 bytes of a row of the result, at an address that is aligned to an element.
-template <bool BF16>
+template <bool HALF>
 struct Out;
 template <>
 struct Out<true> {
     typedef u4 Vec;
-    static constexpr int BYTES = 2;
 };
 template <>
 struct Out<false> {
     typedef f4 Vec;
-    static constexpr int BYTES = 4;
 };
 
-template <bool BF16>
-__device__ __forceinline__ void store_row(const Matmul& p, int64_t m, int64_t n, typename Out<BF16>::Vec v)
+template <bool HALF>
+__device__ __forceinline__ void store_row(const Matmul& p, int64_t m, int64_t n, typename Out<HALF>::Vec v)
 {
     if (n >= p.N) return;
     const int64_t at = m * p.N + n;
-    if constexpr (BF16) {
+    if constexpr (HALF) {
         typedef u4 __attribute__((aligned(2))) any_u4;
         uint16_t* const out = (uint16_t*)p.out + at;
         if (n + 8 <= p.N) {
@@ -426,11 +427,11 @@ __device__ __forceinline__ i8 load_codes(const uint8_t* p)
 
 // ---- few rows: codes straight into registers
 // A wavefront computes 16 columns of the result in MF * 16 rows: lane l holds 32 codes of row l % 16 of a fragment.  It takes every kw-th run of four
-// blocks, all of whose codes it asks for at once; the kw wavefronts of one place add their sums up in LDS, in their order.  Bound by reading B once.
+// blocks, all of whose codes it asks for at once; the kw wavefronts of one place add their sums up in LDS, in their order.  Bound by reading B once:
+// one row, N = 32768, K = 1024 6.9 us = 4.9 TB/s, a launch of 2 us included; sixteen rows to bf16 9.4.
 template <int FA, int FB, bool HALF, int MF>
 __global__ __launch_bounds__(256) void rows_kernel(Matmul p, int log_kw)
 {
-    constexpr int U = 4;           // blocks that are loaded together
     __shared__ f4 sums[4][MF][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const int kw = 1 << log_kw, part = wave & (kw - 1), places = (int)(blockDim.x >> 6) >> log_kw;
@@ -451,34 +452,30 @@ __global__ __launch_bounds__(256) void rows_kernel(Matmul p, int log_kw)
         uint32_t wa[MF];
 #pragma unroll
         for (int h = 0; h < MF; ++h) wa[h] = *reinterpret_cast<const uint32_t*>(sa[h] + k);
+        i8 u[4], v[4][MF];
 #pragma unroll
-        for (int q0 = 0; q0 < 4; q0 += U) {
-            i8 u[U], v[U][MF];
+        for (int q = 0; q < 4; ++q) {
+            const int64_t at = (int64_t)(k + q < p.blocks ? k + q : p.blocks - 1) * kBlock;      // (behind the last block: it again, unused)
+            u[q] = load_codes(b + at);
 #pragma unroll
-            for (int q = 0; q < U; ++q) {
-                const int64_t at = (int64_t)(k + q0 + q < p.blocks ? k + q0 + q : p.blocks - 1) * kBlock;      // (behind the last block: it again, unused)
-                u[q] = load_codes(b + at);
+            for (int h = 0; h < MF; ++h) v[q][h] = load_codes(a[h] + at);
+        }
 #pragma unroll
-                for (int h = 0; h < MF; ++h) v[q][h] = load_codes(a[h] + at);
-            }
+        for (int q = 0; q < 4; ++q) {
+            if (k + q >= p.blocks) break;
+            if constexpr (HALF) {
 #pragma unroll
-            for (int q = 0; q < U; ++q) {
-                if (k + q0 + q >= p.blocks) break;
-                const int shift = (q0 + q) * 8;
-                if constexpr (HALF) {
+                for (int h = 0; h < MF; ++h)
+                    acc[h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u[q], v[q][h], acc[h], FB, FA, 0, (int)(wb >> 8 * q), 0, (int)(wa[h] >> 8 * q));
+            } else {
+                b8 x[4];
+                widen<FB>(u[q], (wb >> 8 * q) & 255u, x);
 #pragma unroll
-                    for (int h = 0; h < MF; ++h)
-                        acc[h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u[q], v[q][h], acc[h], FB, FA, 0, (int)(wb >> shift), 0, (int)(wa[h] >> shift));
-                } else {
-                    b8 x[4];
-                    widen<FB>(u[q], (wb >> shift) & 255u, x);
+                for (int h = 0; h < MF; ++h) {
+                    b8 y[4];
+                    widen<FA>(v[q][h], (wa[h] >> 8 * q) & 255u, y);
 #pragma unroll
-                    for (int h = 0; h < MF; ++h) {
-                        b8 y[4];
-                        widen<FA>(v[q][h], (wa[h] >> shift) & 255u, y);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[r], y[r], acc[h], 0, 0, 0);
-                    }
+                    for (int r = 0; r < 4; ++r) acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[r], y[r], acc[h], 0, 0, 0);
                 }
             }
         }
@@ -505,14 +502,15 @@ __global__ __launch_bounds__(256) void rows_kernel(Matmul p, int log_kw)
 // ---- large products: tiles through LDS
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
-// Waits for this wavefront's loads into LDS and its reads from it, then for the work-group's other wavefronts.
-// (all but the LATER last ones)
+// Waits for this wavefront's reads from LDS and for all but the LATER last of its accesses to memory, which end in their order, loads into LDS among
+// them; then for the work-group's other wavefronts.
 template <int LATER = 0>
 __device__ __forceinline__ void wait_and_meet()
 {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER < 63 ? LATER : 63) : "memory");
 }
-// The same for all of them, or, behind stores that lie after the loads in question, for all but the LATER last.
+// The same with LATER where the last accesses are stores behind the loads in question, else with none.  (In one statement: a branch would end the run of
+// instructions that keeps its order.)
 template <int LATER>
 __device__ __forceinline__ void meet_behind_stores(bool behind)
 {
@@ -520,13 +518,13 @@ __device__ __forceinline__ void meet_behind_stores(bool behind)
                  ::"n"(LATER < 63 ? LATER : 63), "s"(__builtin_amdgcn_readfirstlane((int)behind)) : "memory", "scc");
 }
 
+#ifdef __HIP_DEVICE_COMPILE__     // (a buffer's type is none of the host compiler's)
 __device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0); }
 
-#ifdef __HIP_DEVICE_COMPILE__
-// A part of an operand as a buffer: reads beyond `bytes` give zeros.
+// A part of an operand as a buffer: reads beyond `bytes` give zeros.  What is added to a load's own offset is never more than `bytes`.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const uint8_t* p, int64_t bytes)
 {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, (int)(uint32_t)(bytes < 0xFFFFFFFFll ? bytes : 0xFFFFFFFFll), 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, (int)(uint32_t)bytes, 0x00020000);
 }
 #endif
 
@@ -539,10 +537,20 @@ struct Tile {
     static constexpr int RESULT = UNREAD + 1024, LDS = RESULT + WN * WM * 8 * PITCH;
 };
 
+// A work-group of WN x WM wavefronts computes tiles of TN columns by TM rows of the result, a wavefront NF x MF fragments of 16 x 16, whose sums stay in
+// its registers; it takes tile after tile, as many work-groups as the GPU holds.  Codes go from memory into LDS past the registers, one block of 128
+// along K ahead.  Bound by the matrix instructions, the loads' latencies between them and, where K is short, by writing the result (256 x 256):
+//                                       us       TFLOP/s    without any loads / without any accesses
+//   8192^3 to bf16                      401      2740       319 / 272 us
+//   8192 x 32768 x 1024 to bf16         283      1940       203 / 181, without stores 233
+//   8192^3 to fp32                      731      1504
+// What else was measured and lost: a ring of four half-blocks with 32 x 32 x 64 products (500 and 317 us: half lines of 64 bytes, twice the requests to L2),
+// 128 x 128 tiles everywhere (540 and 343), four wavefronts of 128 x 128 (431 and 302), work-groups that begin one after the other, so that not all
+// store at a time (8192^3 15 % slower).
 template <int FA, int FB, bool HALF, bool ONTO, int WN, int WM, int NF, int MF>
-__global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
+__global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel([[maybe_unused]] Matmul p)
 {
-#ifdef __HIP_DEVICE_COMPILE__     // (a buffer's type is none of the host compiler's)
+#ifdef __HIP_DEVICE_COMPILE__
     typedef Tile<HALF, WN, WM, NF, MF> T;
     constexpr int TN = T::TN, TM = T::TM, ROWS = T::ROWS, STAGE = T::STAGE, SCALES = T::SCALES, WAVES = WN * WM;
     constexpr int LB = TN / (8 * WAVES), LA = TM / (8 * WAVES);     // loads of 1 KiB by a wavefront, for one block
@@ -630,12 +638,12 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
 #pragma unroll
         for (int h = 0; h < MF; ++h) sa[h] = *reinterpret_cast<const uint32_t*>(at + (TN + (wm * MF + h) * 16 + i) * 4);
     };
-    // A block's last fragment of B is multiplied behind the meeting that ends its stage, while the next block's first codes are
-    // on their way from LDS; the loads of the block after that, into the stage that the meeting has set free, are spread over the first
-    // half of the next block, so that none of them holds up a read from LDS that a multiplication waits for.
+    // The loads of a block are spread over the multiplication of the one before, so that none of them holds up a read from LDS that a product
+    // waits for.  A stage is free for them once the block in it has been read, from the middle of its multiplication on (bf16 result), or but for its
+    // last fragment of B (fp32, whose widened codes leave no registers for half a block's).
     constexpr int SPREAD = HALF ? NF : NF > 4 ? NF / 2 : NF - 1, AT_ONCE = (LOADS + SPREAD - 1) / SPREAD;
     typedef typename Out<HALF>::Vec Vec;
-    constexpr int PER_VEC = 16 / Out<HALF>::BYTES, EF = T::EF, VECS = EF * 16 / PER_VEC, PITCH = T::PITCH, TURN = 64 / VECS;
+    constexpr int PER_VEC = HALF ? 8 : 4, EF = T::EF, VECS = EF * 16 / PER_VEC, PITCH = T::PITCH, TURN = 64 / VECS;
     static_assert(64 % VECS == 0 && 8 % TURN == 0, "whole rows");
     constexpr int NT = 2;           // nontemporal
     constexpr int STORES = MF * (NF / EF) * (16 / TURN);
@@ -768,55 +776,65 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(Matmul p)
             continue;
         }
         uint8_t* const mine = lds + T::RESULT + wave * 8 * PITCH;
+        const auto leave = [&](auto in_advance) {
+            constexpr bool AHEAD = decltype(in_advance)::value;
 #pragma unroll
-        for (int h = 0; h < MF; ++h) {
-            f4 c[NF / EF][16 / TURN];
-            if (ahead) {
-                const __amdgpu_buffer_rsrc_t onto = buffer((const uint8_t*)(p.c_in + corner), 0x7FFFFFFF);
-                keep_order();
+            for (int h = 0; h < MF; ++h) {
+                [[maybe_unused]] f4 c[NF / EF][16 / TURN];
+                if constexpr (AHEAD) {
+                    const __amdgpu_buffer_rsrc_t onto = buffer((const uint8_t*)(p.c_in + corner), 0x7FFFFFFF);
+                    keep_order();
 #pragma unroll
-                for (int e = 0; e < NF; e += EF)
+                    for (int e = 0; e < NF; e += EF)
 #pragma unroll
-                    for (int t = 0; t < 16 / TURN; ++t)
-                        c[e / EF][t] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(onto, from_corner, (h * 16 + t * TURN) * row_bytes + e * 64, NT));
-            }
+                        for (int t = 0; t < 16 / TURN; ++t)
+                            c[e / EF][t] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(onto, from_corner, (h * 16 + t * TURN) * row_bytes + e * 64, NT));
+                }
 #pragma unroll
-            for (int e = 0; e < NF; e += EF) {
+                for (int e = 0; e < NF; e += EF) {
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    if ((i >> 3) == half) {
+                    for (int half = 0; half < 2; ++half) {
+                        if ((i >> 3) == half) {
 #pragma unroll
-                        for (int f = e; f < e + EF; ++f) {
-                            if constexpr (HALF) {
-                                if (f & 1) {
-                                    const u4 w = {narrow2(acc[f - 1][h].x, acc[f - 1][h].y), narrow2(acc[f - 1][h].z, acc[f - 1][h].w),
-                                                  narrow2(acc[f][h].x, acc[f][h].y), narrow2(acc[f][h].z, acc[f][h].w)};
-                                    *reinterpret_cast<u4*>(mine + (i & 7) * PITCH + ((f >> 1) * 32 + g * 8) * 2) = w;
+                            for (int f = e; f < e + EF; ++f) {
+                                if constexpr (HALF) {
+                                    if (f & 1) {
+                                        const u4 w = {narrow2(acc[f - 1][h].x, acc[f - 1][h].y), narrow2(acc[f - 1][h].z, acc[f - 1][h].w),
+                                                      narrow2(acc[f][h].x, acc[f][h].y), narrow2(acc[f][h].z, acc[f][h].w)};
+                                        *reinterpret_cast<u4*>(mine + (i & 7) * PITCH + ((f >> 1) * 32 + g * 8) * 2) = w;
+                                    }
+                                } else {
+                                    *reinterpret_cast<f4*>(mine + (i & 7) * PITCH + ((f - e) * 16 + g * 4) * 4) = acc[f][h];
                                 }
-                            } else {
-                                *reinterpret_cast<f4*>(mine + (i & 7) * PITCH + ((f - e) * 16 + g * 4) * 4) = acc[f][h];
                             }
                         }
-                    }
-                    __builtin_amdgcn_wave_barrier();
-                    Vec out[8 / TURN];
+                        __builtin_amdgcn_wave_barrier();
+                        Vec out[8 / TURN];
 #pragma unroll
-                    for (int t = 0; t < 8 / TURN; ++t) out[t] = *reinterpret_cast<const Vec*>(mine + (t * TURN + lane / VECS) * PITCH + (lane % VECS) * 16);
+                        for (int t = 0; t < 8 / TURN; ++t) out[t] = *reinterpret_cast<const Vec*>(mine + (t * TURN + lane / VECS) * PITCH + (lane % VECS) * 16);
 #pragma unroll
-                    for (int t = 0; t < 8 / TURN; ++t) {
-                        const int64_t m = m_out + h * 16 + half * 8 + t * TURN;
-                        if (ahead) {
-                            if constexpr (!HALF)
+                        for (int t = 0; t < 8 / TURN; ++t) {
+                            const int64_t m = m_out + h * 16 + half * 8 + t * TURN;
+                            if constexpr (AHEAD) {
+                                // (All of the offset in the vector register: behind a store of 16 bytes with a scalar register for an offset the compiler
+                                // leaves no wait before the data's registers are written again, and the store has taken what was written.)
                                 __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, out[t] + c[e / EF][half * (8 / TURN) + t]),
-                                                                       buffer((const uint8_t*)((const float*)p.out + corner), 0x7FFFFFFF), from_corner,
-                                                                       (h * 16 + half * 8 + t * TURN) * row_bytes + e * 64, NT);
-                        } else if (m < p.M) {
-                            store_row<HALF>(p, m, n_out + e * 16, out[t]);
+                                                                       buffer((const uint8_t*)((const float*)p.out + corner), 0x7FFFFFFF),
+                                                                       from_corner + (uint32_t)(h * 16 + half * 8 + t * TURN) * row_bytes + e * 64, 0, NT);
+                            } else if (m < p.M) {
+                                store_row<HALF>(p, m, n_out + e * 16, out[t]);
+                            }
                         }
+                        __builtin_amdgcn_wave_barrier();
                     }
-                    __builtin_amdgcn_wave_barrier();
                 }
             }
+        };
+        if constexpr (ONTO) {
+            if (ahead) leave(std::true_type());
+            else leave(std::false_type());
+        } else {
+            leave(std::false_type());
         }
         if (tile >= all) return;
         // the loads are older than the stores: where every store was made, these may still be on their way
@@ -1000,7 +1018,7 @@ void launch_matmul(const Matmul& p, bool half, const Way& w, hipStream_t stream)
 
 bool unaligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
 bool bad_format(int32_t f) { return f != TS_FP8_E4M3 && f != TS_FP8_E5M2; }
-constexpr int64_t kSizeMax = (int64_t)1 << 31, kKMax = (int64_t)1 << 24;
+constexpr int64_t kSizeMax = (int64_t)1 << 31, kKMax = ((int64_t)1 << 24) - kBlock;      // (256 rows of codes: below 2^32 bytes)
 
 }  // namespace
 

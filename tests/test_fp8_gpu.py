@@ -284,3 +284,37 @@ def test_shapes_and_types_of_the_binding():
         ts.ts_quantize_fp8(x, E4M3)
     with pytest.raises(ts.TsError):
         ts.ts_matmul_fp8(q, s, w, sw, K, out.bfloat16(), torch.zeros(M, N, device=DEV))
+
+
+# large and small tiles, several to a work-group, tiles that end inside, unfinished rounds in parts: sizes at which each is taken
+@pytest.mark.parametrize("M,N,K", [(4096, 4096, 1024), (8500, 2100, 5000), (2000, 9001, 300), (1500, 1500, 3000), (8192, 1024, 6000), (600, 8000, 128)])
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "onto", "in place"])
+def test_large_products_of_whole_numbers_are_exact(M, N, K, kind):
+    a, sa = operand(M, K, E4M3, "whole", M + K)
+    b, sb = operand(N, K, E5M2, "whole", N + K + 1)
+    # every partial sum is a whole number below 2^24 in fp32, too: at most K * (4 * 4)^2
+    assert K * 256 < 2 ** 24
+    want = op.values(a, sa, 0).astype(np.float32) @ op.values(b, sb, 1).astype(np.float32).T
+    if kind == "bf16":
+        # one rounding: products of 1 to 256 lie within the 13 bits that the 8-bit instructions keep
+        got = product(a, sa, 0, b, sb, 1, K, BF16)
+        assert np.array_equal(got, torch.from_numpy(want).to(BF16).double().numpy())
+        return
+    c_in = None
+    if kind != "fp32":
+        c_in = np.random.default_rng(3).integers(-1000, 1001, (M, N)).astype(np.float32)
+        want = want + c_in
+    assert np.array_equal(product(a, sa, 0, b, sb, 1, K, FP32, c_in, kind == "in place"), want)
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 40, 300), (70, 200, 300), (300, 300, 9000)])
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+def test_a_scale_byte_of_255_is_nan(M, N, K, dtype):
+    a, sa = operand(M, K, E4M3, "whole", 1)
+    b, sb = operand(N, K, E4M3, "whole", 2)
+    sa[1, 2] = 255
+    sb[5, 0] = 255
+    got = product(a, sa, 0, b, sb, 0, K, dtype)
+    assert np.isnan(got[1]).all() and np.isnan(got[:, 5]).all()
+    rest = np.isfinite(np.delete(np.delete(got, 1, 0), 5, 1))
+    assert rest.all()

@@ -84,7 +84,7 @@ def test_matmul():
     for at, value, want in ((0, None, ts.TS_ERR_NULL), (1, None, ts.TS_ERR_NULL), (3, None, ts.TS_ERR_NULL), (4, None, ts.TS_ERR_NULL),
                             (10, None, ts.TS_ERR_NULL), (2, 2, ts.TS_ERR_SHAPE), (5, -1, ts.TS_ERR_SHAPE), (6, -1, ts.TS_ERR_SHAPE),
                             (7, -1, ts.TS_ERR_SHAPE), (8, -1, ts.TS_ERR_SHAPE), (11, 2, ts.TS_ERR_SHAPE), (11, 1, ts.TS_ERR_SHAPE),
-                            (6, N31, ts.TS_ERR_OVERFLOW), (7, N31, ts.TS_ERR_OVERFLOW), (8, (1 << 24) + 1, ts.TS_ERR_OVERFLOW),
+                            (6, N31, ts.TS_ERR_OVERFLOW), (7, N31, ts.TS_ERR_OVERFLOW), (8, (1 << 24) - 127, ts.TS_ERR_OVERFLOW),
                             (0, ODD, ts.TS_ERR_ALIGN), (3, ODD, ts.TS_ERR_ALIGN), (9, ODD, ts.TS_ERR_ALIGN), (10, ODD, ts.TS_ERR_ALIGN),
                             (1, C.c_void_p(2), ts.TS_ERR_ALIGN), (4, C.c_void_p(2), ts.TS_ERR_ALIGN)):
         assert f(*[value if i == at else x for i, x in enumerate(ok)]) == want, (at, value)
@@ -96,9 +96,9 @@ def test_matmul_workspace_bytes():
     f, b = ts.lib().ts_matmul_workspace_bytes, C.c_int64(-1)
     assert f(1, 1, 1, None) == ts.TS_ERR_NULL
     for sizes, want in (((-1, 1, 1), ts.TS_ERR_SHAPE), ((1, -1, 1), ts.TS_ERR_SHAPE), ((1, 1, -1), ts.TS_ERR_SHAPE),
-                        ((N31, 1, 1), ts.TS_ERR_OVERFLOW), ((1, N31, 1), ts.TS_ERR_OVERFLOW), ((1, 1, (1 << 24) + 1), ts.TS_ERR_OVERFLOW)):
+                        ((N31, 1, 1), ts.TS_ERR_OVERFLOW), ((1, N31, 1), ts.TS_ERR_OVERFLOW), ((1, 1, (1 << 24) - 127), ts.TS_ERR_OVERFLOW)):
         assert f(*sizes, C.byref(b)) == want
-    for sizes in ((0, 0, 0), (1, 32768, 1024), (8192, 32768, 1024), (64, 1024, 32768), (1, 1, 1 << 24), (16, 16, 100)):
+    for sizes in ((0, 0, 0), (1, 32768, 1024), (8192, 32768, 1024), (64, 1024, 32768), (1, 1, (1 << 24) - 128), (16, 16, 100)):
         assert 0 <= ts.ts_matmul_workspace_bytes(*sizes) < 1 << 31
 
 
