@@ -49,7 +49,9 @@ __device__ __forceinline__ void store4(uint16_t* p, f4 v)
     __builtin_nontemporal_store(b, reinterpret_cast<u2*>(p));
 }
 
-// out[e] = add[e] + (kept ? x[e] * factor : 0) over a flat array, four elements per lane.
+// out[e] = add[e] + (kept ? x[e] * factor : 0) over a flat array, four elements per lane: those of one counter, so that no bit is made twice and no
+// lane waits for another.  Bound by memory: nothing is read again, so all accesses are nontemporal.  With a residual, 65536 x 1024 bf16 66.5 us =
+// 6.1 TB/s (a copy kernel reaches 6.2 to 6.4 here), 4987 x 516 fp32 6.2 us, of which 2 are the launch.
 template <typename T, bool ADD>
 __global__ __launch_bounds__(kThreads) void dropout_kernel(const T* x, const T* add, T* out, int64_t groups, int64_t g_first, Mask m)
 {
@@ -70,7 +72,10 @@ struct Lookup {
 };
 
 // out[t] = dropout(scale * weight[ids[t]] + pos[pos_ids[t]]).  A row belongs to `lanes` neighbouring lanes (a power of two), a
-// work-group takes 4 * 64 / lanes rows and, where rows are wider than 64 lanes, one block of CH * 256 of their columns.
+// work-group takes 4 * 64 / lanes rows and, where rows are wider than 64 lanes, one block of CH * 256 of their columns: a lane then asks for all its
+// parts of a row before it needs one (rows' addresses come from ids, which is a second latency).  Bound by memory: 16384 rows of 1024 from an fp32
+// weight of 32768 rows, positions and a bf16 result 12.7 us = 7 TB/s with rows that repeat read from the cache (28 us with one load per lane in
+// flight); one row 4.3 us, a launch.
 template <typename W, typename O, int CH>
 __global__ __launch_bounds__(kThreads) void lookup_kernel(Lookup p, int log_lanes)
 {
