@@ -293,3 +293,16 @@ def test_streams_and_shapes_of_the_binding():
             ts.ts_dropout(x, mask, out)
     with pytest.raises(ts.TsError):
         ts.ts_dropout(x, ts.DropoutMask(1.0, 1), out)
+
+
+def test_elements_beyond_2_to_the_34():
+    """Groups of four beyond 2^32: the counter's second word."""
+    d, rows = 1 << 20, (1 << 14) + 2
+    x = torch.empty(rows, d, dtype=BF16, device=DEV)                  # 34 GB, of which the ends are looked at
+    x[0].fill_(1.0)
+    x[-2:].fill_(1.0)
+    ts.ts_dropout(x, ts.DropoutMask(0.5, 9, 1), x)
+    for first, part in ((0, x[:1]), (rows - 2, x[-2:])):
+        assert np.array_equal(host(part) == 2.0, op.kept(part.shape[0], d, 0.5, 9, 1, first_row=first))
+    del x
+    torch.cuda.empty_cache()
