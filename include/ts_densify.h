@@ -219,7 +219,8 @@ int ts_densify_dropout(const int32_t* ids, const void* rows, int64_t n, int32_t 
  * An operand [rows, K] is held as codes [rows, K rounded up to 128], one byte each (OCP e4m3 without infinities, or
  * e5m2), what is beyond K zero, and as scales, one byte s for each block of 128 codes of a row, whose values are then
  * code * 2^(s - 127): [rows, number of blocks rounded up to 4], bytes beyond the last block zero.  Both are row-major
- * and contiguous; ts_fp8_layout returns the two row lengths.
+ * and contiguous; ts_fp8_layout returns the two row lengths.  Such values are in fp32's range if ts_quantize_fp8 made them;
+ * of others, those of 2^128 and more may count as infinite, and those below 2^-126 lose what lies below 2^-133.
  */
 enum { TS_FP8_E4M3 = 0, TS_FP8_E5M2 = 1 };
 #define TS_FP8_BLOCK 128

@@ -306,3 +306,49 @@ def test_elements_beyond_2_to_the_34():
         assert np.array_equal(host(part) == 2.0, op.kept(part.shape[0], d, 0.5, 9, 1, first_row=first))
     del x
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("n,d,V,used", [(2048, 64, 1000, 2048), (20000, 260, 5000, 20000), (70000, 1024, 9000, 70000), ((1 << 22) + 100, 4096, 1000, 100)])
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+def test_densify_dropout_is_densify_of_dropped_rows(n, d, V, used, dtype):
+    """Bit for bit with a factor of two, which rounds nothing.  The last rows lie beyond 2^34 elements, the others are padding."""
+    if dtype == FP32 and n > 1 << 20:
+        n = n // 4 + 75
+    rows = torch.empty(n, d, dtype=dtype, device=DEV)
+    rows[n - used:] = torch.randn(used, d, generator=torch.Generator().manual_seed(n)).to(dtype).to(DEV)
+    ids = torch.full((n,), -1, dtype=torch.int32, device=DEV)
+    ids[n - used:] = torch.randint(0, V, (used,), generator=torch.Generator().manual_seed(d), dtype=torch.int32).to(DEV)
+    dense = values((V, d), FP32).to(DEV)
+    got, want = torch.empty_like(dense), torch.empty_like(dense)
+    ws = torch.empty(ts.ts_workspace_bytes(n, d, V), dtype=torch.uint8, device=DEV)
+    m = ts.DropoutMask(0.5, SEED, OFFSET)
+    ts.ts_bind_workspace(ws)
+    try:
+        ts.ts_densify_dropout(ids, rows, d, V, 1.0, m, dense, got)
+        ts.ts_dropout(rows, m, rows)
+        (ts.ts_densify_bf16 if dtype == BF16 else ts.ts_densify)(ids, rows, d, V, dense, want)
+        torch.cuda.synchronize()
+    finally:
+        ts.ts_bind_workspace(None)
+    assert torch.equal(got.view(torch.int32), want.view(torch.int32))
+    assert not torch.equal(got, dense)
+    del rows
+    torch.cuda.empty_cache()
+
+
+def test_lookup_beyond_2_to_the_32():
+    """Rows of a weight, and of the result, behind 2^32 elements."""
+    d, V = 4096, (1 << 20) + 40
+    weight = torch.empty(V, d, dtype=BF16, device=DEV)
+    weight[-40:] = values((40, d), BF16).to(DEV)
+    n = (1 << 20) + 9
+    ids = torch.full((n,), -1, dtype=torch.int32, device=DEV)
+    last = torch.arange(V - 20, V - 11, dtype=torch.int32)
+    ids[-9:] = last.to(DEV)
+    out = torch.empty(n, d, dtype=BF16, device=DEV)
+    ts.ts_lookup_dropout(ids, weight, 2.0, ts.DropoutMask(0.25, SEED, OFFSET), out)
+    keep = op.kept(9, d, 0.25, SEED, OFFSET, first_row=n - 9)
+    near(out[-9:], np.where(keep, host(weight[-20:-11]) * 2.0 / 0.75, 0.0), BF16, 2)
+    assert not bool(out[:-9].any())
+    del weight, out
+    torch.cuda.empty_cache()

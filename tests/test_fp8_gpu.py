@@ -318,3 +318,77 @@ def test_a_scale_byte_of_255_is_nan(M, N, K, dtype):
     assert np.isnan(got[1]).all() and np.isnan(got[:, 5]).all()
     rest = np.isfinite(np.delete(np.delete(got, 1, 0), 5, 1))
     assert rest.all()
+
+
+def test_codes_beyond_2_to_the_32():
+    """Codes, of both ways, behind 2^32 bytes."""
+    rows, cols = 66000, 65700
+    x = torch.zeros(rows, cols, dtype=BF16, device=DEV)
+    g = torch.Generator().manual_seed(1)
+    x[-140:] = torch.randn(140, cols, generator=g).to(BF16).to(DEV)
+    x[:, -140:] = torch.randn(rows, 140, generator=g).to(BF16).to(DEV)
+    q, s, qt, st = quantized(x, E4M3)
+    for codes, scales, of in ((q[-140:], s[-140:], x[-140:]), (qt[-140:], st[-140:], x[:, -140:].T)):
+        want, want_scales = op.quantize(of.float().cpu().numpy(), E4M3)
+        assert np.array_equal(scales.cpu().numpy(), want_scales)
+        same_codes(codes, want, E4M3)
+    del x, q, qt
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("M,N", [(66000, 65700), (20, 230000000)])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_results_beyond_2_to_the_32(M, N, dtype):
+    """Elements behind 2^32, of whole numbers; few rows and many."""
+    K, far = 100, 300
+    b, sb = operand(far, K, E4M3, "whole", 2)
+    a, sa = operand(min(M, far), K, E4M3, "whole", 3)
+    qa, ssa = ts.fp8_empty(M, K)
+    qb, ssb = ts.fp8_empty(N, K)
+    for t in (qa, qb):
+        t.view(torch.uint8).zero_()
+    for t in (ssa, ssb):
+        t.zero_()
+    qa.view(torch.uint8)[-len(a):], ssa[-len(a):] = torch.from_numpy(a).to(DEV), torch.from_numpy(sa).to(DEV)
+    qb.view(torch.uint8)[-far:], ssb[-far:] = torch.from_numpy(b).to(DEV), torch.from_numpy(sb).to(DEV)
+    out = torch.full((M, N), 3.0, dtype=dtype, device=DEV)
+    c_in = out if dtype == FP32 else None
+    ws = bind(M, N, K)
+    try:
+        ts.ts_matmul_fp8(qa, ssa, qb, ssb, K, out, c_in)
+        torch.cuda.synchronize()
+    finally:
+        ts.ts_bind_workspace(None)
+        del ws
+    want = op.values(a, sa, 0) @ op.values(b, sb, 0).T
+    got = out[-len(a):, -far:].double().cpu()
+    if dtype == BF16:
+        assert torch.equal(got, torch.from_numpy(want).to(BF16).double())
+    else:
+        assert np.array_equal(got.numpy(), want + 3.0)
+    rest = 0.0 if dtype == BF16 else 3.0
+    assert bool((out[:, :-far] == rest).all())
+    del out, c_in, qa, qb
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 40, 300), (200, 300, 500)])
+@pytest.mark.parametrize("low,high", [(0, 230), (1, 140), (3, 250), (254, 20), (254, 0)])
+def test_scales_at_the_ends(M, N, K, low, high):
+    """The smallest and the largest bytes; codes of 1 to 1.75, so that every value and every result is one that fp32 holds."""
+    rng = np.random.default_rng(low)
+    blocks = -(-K // 128)
+    ops = []
+    for rows, byte in ((M, low), (N, high)):
+        codes, scales = np.zeros((rows, blocks * 128), np.uint8), np.zeros((rows, -(-blocks // 4) * 4), np.uint8)
+        codes[:, :K] = op.encode(rng.integers(4, 8, (rows, K)) / 4.0, E4M3)
+        scales[:, :blocks] = byte
+        ops += [codes, scales]
+    a, sa, b, sb = ops
+    want = op.values(a, sa, 0) @ op.values(b, sb, 0).T             # whole multiples of 1/16 of a power of two, sums below 2^12 of them
+    if np.abs(want).max() < 2.0 ** 127 and np.abs(want).max() >= 2.0 ** -110:
+        assert np.array_equal(product(a, sa, 0, b, sb, 0, K, FP32), want)
+        got = product(a, sa, 0, b, sb, 0, K, BF16)
+        assert np.array_equal(got, torch.from_numpy(want).to(BF16).double().numpy())
+    else:
+        raise AssertionError("not a case")
