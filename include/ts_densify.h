@@ -232,7 +232,8 @@ int ts_fp8_layout(int64_t K, int64_t* code_bytes, int64_t* scale_bytes);
  * pair may be NULL, not both.  The scale of a block is the smallest power of two, 2^-127 at least, that brings its
  * largest finite magnitude to at most 448 (e4m3) or 57344 (e5m2); codes are rounded to nearest, ties to even, so no
  * finite value becomes infinite.  NaN stays NaN; an infinity becomes NaN in e4m3 and stays one in e5m2.  q, qt: 16-byte
- * aligned, scales: 4-byte aligned, x: 16-byte aligned; rows or cols may be 0 (then nothing is written).
+ * aligned, scales: 4-byte aligned, x: 16-byte aligned; rows or cols may be 0 (then nothing is read or written).  Outputs
+ * must not overlap x or each other.
  */
 int ts_quantize_fp8(const void* x, int32_t x_dtype, int64_t rows, int64_t cols, int32_t format,
                     uint8_t* q, uint8_t* q_scales, uint8_t* qt, uint8_t* qt_scales, void* stream);
@@ -245,10 +246,11 @@ int ts_quantize_fp8(const void* x, int32_t x_dtype, int64_t rows, int64_t cols, 
  * [M, N] is TS_OUT_FP32, made from exact products, or TS_OUT_BF16, made by the 8-bit matrix instructions, which cut what a
  * product has more than 13 bits below the largest of its group of eight along K (1.5e-5 of the result's norm on normal
  * data), and rounded once; c_in must be NULL with TS_OUT_BF16, else TS_ERR_SHAPE.  c_in fp32 [M, N] or NULL; it may be
- * out.  M, N or K may be 0 (K = 0: out = c_in or zeros).  a, b: 16-byte aligned, scales: 4-byte, out and c_in: 16-byte.  M, N
- * below 2^31, K at most 2^24 - 128.
- * A product of few rows and columns is split along K and uses the bound workspace, ts_matmul_workspace_bytes(M, N, K)
- * bytes of it (0 where it is not split); what ts_last_views described in that workspace is then gone.
+ * out; other overlaps are undefined.  M, N or K may be 0 (K = 0: out = c_in or zeros).  a, b: 16-byte aligned, scales:
+ * 4-byte, out and c_in: 16-byte.  M, N below 2^31, K at most 2^24 - 128.
+ * A product whose tiles would leave part of the GPU without work is split along K and uses the bound workspace,
+ * ts_matmul_workspace_bytes(M, N, K) bytes of it (0 where it is not split); what ts_last_views described in that
+ * workspace is then gone.
  */
 int ts_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t* bytes);
 int ts_matmul_fp8(const uint8_t* a, const uint8_t* a_scales, int32_t a_format,

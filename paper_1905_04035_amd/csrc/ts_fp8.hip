@@ -1039,9 +1039,9 @@ int ts_quantize_fp8(const void* x, int32_t x_dtype, int64_t rows, int64_t cols, 
 {
     if (rows < 0 || cols < 0 || bad_format(format) || (x_dtype != TS_ROW_FP32 && x_dtype != TS_ROW_BF16)) return TS_ERR_SHAPE;
     if (rows >= kSizeMax || cols >= kSizeMax) return TS_ERR_OVERFLOW;
+    if (rows == 0 || cols == 0) return TS_OK;           // (an empty tensor has no address)
     if ((!q && !qt) || (!q != !q_scales) || (!qt != !qt_scales)) return TS_ERR_NULL;
     if (unaligned(x, 16) || unaligned(q, 16) || unaligned(qt, 16) || unaligned(q_scales, 4) || unaligned(qt_scales, 4)) return TS_ERR_ALIGN;
-    if (rows == 0 || cols == 0) return TS_OK;
     if (!x) return TS_ERR_NULL;
     Quantize p;
     p.x = x;

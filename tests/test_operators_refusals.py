@@ -76,6 +76,8 @@ def test_quantize():
         assert f(*[value if i == at else x for i, x in enumerate(ok)]) == want, (at, value)
     assert f(P, 0, 8, 16, 0, None, None, None, None, None) == ts.TS_ERR_NULL
     assert f(None, 0, 0, 16, 0, P, P, None, None, None) == ts.TS_OK and f(None, 0, 8, 0, 0, None, None, P, P, None) == ts.TS_OK
+    assert f(None, 0, 0, 0, 0, P, P, None, None, None) == ts.TS_OK and f(None, 0, 8, 0, 2, P, P, None, None, None) == ts.TS_ERR_SHAPE
+    assert f(None, 0, 8, 0, 0, None, None, None, None, None) == ts.TS_OK          # (empty tensors have no addresses)
 
 
 def test_matmul():
