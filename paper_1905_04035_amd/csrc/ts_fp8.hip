@@ -82,10 +82,13 @@ __device__ __forceinline__ uint32_t largest_of_16(uint32_t x)
     return larger(x, rotated<1>(x));
 }
 // The largest of lanes i, i + 16, i + 32 and i + 48.
+template <int WIDE>
 __device__ __forceinline__ uint32_t largest_of_rows(uint32_t x)
 {
-    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    x = larger(a[0], a[1]);
+    if constexpr (WIDE == 1) {
+        const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        x = larger(a[0], a[1]);
+    }
     const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
     return larger(b[0], b[1]);
 }
@@ -114,7 +117,8 @@ struct Quantize {
     int64_t row_tiles, col_tiles;
 };
 
-// Eight rows of eight elements as they lie in memory, zeros beyond the matrix; and the bits of the largest magnitudes of a row and of all columns,
+// Eight rows of eight elements as they lie in memory, at any address that is aligned to one, zeros beyond the matrix (WHOLE: a row's length is a multiple of eight);
+// and the bits of the largest magnitudes of a row and of all columns,
 // which show whether a value is no finite number.
 template <typename T>
 struct Part;
@@ -123,19 +127,18 @@ template <>
 struct Part<float> {
     f4 v[8][2];
 
-    template <int VEC>
+    template <bool WHOLE>
     __device__ __forceinline__ void load(int i, const float* p, int64_t left)
     {
+        typedef f4 __attribute__((aligned(4))) any_f4;
+        v[i][0] = v[i][1] = (f4)(0.0f);
+        if (left >= 8) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            v[i][h] = (f4)(0.0f);
-            if (VEC >= 4) {
-                if (4 * h < left) v[i][h] = __builtin_nontemporal_load(reinterpret_cast<const f4*>(p) + h);
-            } else {
+            for (int h = 0; h < 2; ++h) v[i][h] = __builtin_nontemporal_load(reinterpret_cast<const any_f4*>(p) + h);
+        } else if (!WHOLE) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (4 * h + j < left) v[i][h][j] = p[4 * h + j];
-            }
+            for (int j = 0; j < 8; ++j)
+                if (j < left) v[i][j >> 2][j & 3] = p[j];
         }
     }
     __device__ __forceinline__ float value(int i, int c) const { return v[i][c >> 2][c & 3]; }
@@ -170,21 +173,14 @@ struct Part<uint16_t> {
     typedef uint16_t h2 __attribute__((ext_vector_type(2)));
     u4 v[8];
 
-    template <int VEC>
+    template <bool WHOLE>
     __device__ __forceinline__ void load(int i, const uint16_t* p, int64_t left)
     {
+        typedef u4 __attribute__((aligned(2))) any_u4;
         v[i] = (u4)(0u);
-        if (VEC == 8) {
-            if (left > 0) v[i] = __builtin_nontemporal_load(reinterpret_cast<const u4*>(p));
-        } else if (VEC == 4) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (4 * h < left) {
-                    const u2 w = __builtin_nontemporal_load(reinterpret_cast<const u2*>(p) + h);
-                    v[i][2 * h] = w.x;
-                    v[i][2 * h + 1] = w.y;
-                }
-        } else {
+        if (left >= 8) {
+            v[i] = __builtin_nontemporal_load(reinterpret_cast<const any_u4*>(p));
+        } else if (!WHOLE) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (j < left) v[i][j >> 1] |= (uint32_t)p[j] << (j & 1) * 16;
@@ -223,23 +219,27 @@ __device__ __forceinline__ uint32_t finite_size(float x)
     return b < kInfinite ? b : 0u;
 }
 
-// A work-group takes a tile of 128 x 128 elements, a thread 8 x 8 of them.  A row's block is in the registers of sixteen
-// neighbouring lanes; a column's in those of every sixteenth thread.  Where a largest magnitude is that of an infinity or NaN, the elements are
+// A work-group takes WIDE tiles of 128 x 128 elements that lie side by side, a thread 8 x 8 elements.  A row's block is in the registers of sixteen
+// neighbouring lanes; a column's in those of every (16 * WIDE)th thread.  Where a largest magnitude is that of an infinity or NaN, the elements are
 // looked at again without them.  Bound by memory, and so by how many tiles a compute unit holds: bf16 elements stay as they are, two to a register.
-// 8192 x 32768 bf16 to e5m2, both ways / rows only: 208 us = 5.2 TB/s / 145 = 5.6 (261 / 181 with fp32 in the registers and every magnitude by itself).
-template <typename T, int FMT, int VEC>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 5 : 4) void quantize_kernel(Quantize p)
+// 8192 x 32768 bf16 to e5m2, both ways / rows only: 203 us = 5.3 TB/s / 142 = 5.7 (261 / 181 with fp32 in the registers and every magnitude by itself).
+// Two tiles, whose stretches are twice as long, against one: 205 / 210 us there, 8320 x 33152 219 / 234; against two below each other 205 / 212 and 219 / 226.
+template <typename T, int FMT, bool WHOLE, int WIDE>
+__global__ __launch_bounds__(256 * WIDE, sizeof(T) == 2 ? 5 : 4) void quantize_kernel(Quantize p)
 {
-    __shared__ __align__(16) uint32_t most_of[4][kBlock];
-    __shared__ __align__(16) uint8_t turned[kBlock][kBlock + 8];
-    int64_t r_tile, c_tile;
-    place<3>(p.tile_first + blockIdx.x, p.row_tiles, p.col_tiles, &r_tile, &c_tile);
+    __shared__ __align__(16) uint32_t most_of[4 * WIDE][WIDE * kBlock];
+    __shared__ __align__(16) uint8_t turned[WIDE * kBlock][kBlock + 8];
+    constexpr int ACROSS = 16 * WIDE;        // threads beside each other
+    int64_t r_tile, c_wide;
+    place<3>(p.tile_first + blockIdx.x, p.row_tiles, (p.col_tiles + WIDE - 1) / WIDE, &r_tile, &c_wide);
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const int r8 = (tid >> 4) * 8, c8 = (tid & 15) * 8;       // the thread's place in the tile
-    const int64_t r0 = r_tile * kBlock + r8, c0 = c_tile * kBlock + c8;
+    const int r8 = tid / ACROSS * 8, c8 = tid % ACROSS * 8;       // the thread's place
+    const int64_t r0 = r_tile * kBlock + r8, c0 = c_wide * (WIDE * kBlock) + c8;
+    const int64_t c_tile = c_wide * WIDE + c8 / kBlock;
+    const bool here = WIDE == 1 || c_tile < p.col_tiles;
     Part<T> x;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x.template load<VEC>(i, (const T*)p.x + (r0 + i) * p.cols + c0, r0 + i < p.rows ? p.cols - c0 : 0);
+    for (int i = 0; i < 8; ++i) x.template load<WHOLE>(i, (const T*)p.x + (r0 + i) * p.cols + c0, r0 + i < p.rows && here ? p.cols - c0 : 0);
     if (p.q) {
         const int64_t ld = code_row(p.cols), lds = scale_row(p.cols);
 #pragma unroll
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 5 : 4) void quantize_kernel(Q
                 most = largest_of_16(most);
             }
             const uint32_t byte = scale_byte<FMT>(most);
-            if (r0 + i < p.rows) {
+            if (r0 + i < p.rows && here) {
                 const u2 w = {codes4<FMT>(x.four(i, 0), byte), codes4<FMT>(x.four(i, 1), byte)};
                 __builtin_nontemporal_store(w, reinterpret_cast<u2*>(p.q + (r0 + i) * ld + c0));
                 // lane 0 of the sixteen writes the block's byte; behind the last block, lanes 1 to 3 the zeros
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 5 : 4) void quantize_kernel(Q
     uint32_t all = 0;
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
-        most[c] = largest_of_rows(most[c]);
+        most[c] = largest_of_rows<WIDE>(most[c]);
         all = larger(all, most[c]);
     }
     if (__any(all >= kInfinite)) {
@@ -277,10 +277,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 5 : 4) void quantize_kernel(Q
             most[c] = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) most[c] = larger(most[c], finite_size(x.value(i, c)));
-            most[c] = largest_of_rows(most[c]);
+            most[c] = largest_of_rows<WIDE>(most[c]);
         }
     }
-    if (lane < 16) {
+    if (lane < ACROSS) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) *reinterpret_cast<u4*>(&most_of[wave][c8 + 4 * h]) = u4{most[4 * h], most[4 * h + 1], most[4 * h + 2], most[4 * h + 3]};
     }
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 5 : 4) void quantize_kernel(Q
     for (int h = 0; h < 2; ++h) {
         u4 m = (u4)(0u);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < 4 * WIDE; ++w) {
             const u4 a = *reinterpret_cast<const u4*>(&most_of[w][c8 + 4 * h]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) m[j] = larger(m[j], a[j]);
@@ -313,9 +313,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 5 : 4) void quantize_kernel(Q
     // eight lanes to a row of 128 codes
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int c = i * 32 + (tid >> 3), at = (tid & 7) * 16;
-        if (c_tile * kBlock + c < p.cols)
-            __builtin_nontemporal_store(__builtin_shufflevector(*reinterpret_cast<const u2*>(&turned[c][at]), *reinterpret_cast<const u2*>(&turned[c][at + 8]), 0, 1, 2, 3), reinterpret_cast<u4*>(p.qt + (c_tile * kBlock + c) * ld + r_tile * kBlock + at));
+        const int c = i * 32 * WIDE + (tid >> 3), at = (tid & 7) * 16;
+        const int64_t row = c_wide * (WIDE * kBlock) + c;
+        const u2 lo = *reinterpret_cast<const u2*>(&turned[c][at]), hi = *reinterpret_cast<const u2*>(&turned[c][at + 8]);
+        if (row < p.cols)
+            __builtin_nontemporal_store(__builtin_shufflevector(lo, hi, 0, 1, 2, 3), reinterpret_cast<u4*>(p.qt + row * ld + r_tile * kBlock + at));
     }
 }
 
@@ -893,15 +895,25 @@ int compute_units()
     return of[dev];
 }
 
-template <typename T, int FMT>
-void launch_quantize(Quantize p, int64_t tiles, hipStream_t stream)
+template <typename T, int FMT, int WIDE>
+void launch_quantize(Quantize p, hipStream_t stream)
 {
-    in_launches(tiles, kMaxWgs, [&](int64_t at, unsigned n) {
+    const dim3 threads(256 * WIDE);
+    in_launches(p.row_tiles * ((p.col_tiles + WIDE - 1) / WIDE), kMaxWgs, [&](int64_t at, unsigned n) {
         p.tile_first = at;
-        if (p.cols % 8 == 0) hipLaunchKernelGGL((quantize_kernel<T, FMT, 8>), dim3(n), dim3(256), 0, stream, p);
-        else if (p.cols % 4 == 0) hipLaunchKernelGGL((quantize_kernel<T, FMT, 4>), dim3(n), dim3(256), 0, stream, p);
-        else hipLaunchKernelGGL((quantize_kernel<T, FMT, 1>), dim3(n), dim3(256), 0, stream, p);
+        if (p.cols % 8 == 0) hipLaunchKernelGGL((quantize_kernel<T, FMT, true, WIDE>), dim3(n), threads, 0, stream, p);
+        else hipLaunchKernelGGL((quantize_kernel<T, FMT, false, WIDE>), dim3(n), threads, 0, stream, p);
     });
+}
+
+// bf16 rows in pairs of tiles once every compute unit has four: both ways 4096 x 4096 15.4 us in pairs, 16.0 in single tiles, 5000 x 6000 29.3 / 30.8, but 4987 x
+// 2048 12.9 / 11.3, and 1021 x 512 rows only 4.4 / 4.1.  fp32 rows have stretches of 512 bytes anyway: 8192 x 8192 87 / 84, 5000 x 6000 47.6 / 45.6.
+template <int FMT>
+void launch_quantize(const Quantize& p, bool half, hipStream_t stream)
+{
+    if (!half) launch_quantize<float, FMT, 1>(p, stream);
+    else if (p.row_tiles * p.col_tiles >= 1024) launch_quantize<uint16_t, FMT, 2>(p, stream);
+    else launch_quantize<uint16_t, FMT, 1>(p, stream);
 }
 
 // How a product is computed.  The form and the number of parts fix the order of additions, so they follow from the sizes and the result's type alone,
@@ -1053,12 +1065,9 @@ int ts_quantize_fp8(const void* x, int32_t x_dtype, int64_t rows, int64_t cols, 
     p.cols = cols;
     p.row_tiles = (rows + kBlock - 1) / kBlock;
     p.col_tiles = (cols + kBlock - 1) / kBlock;
-    const int64_t tiles = p.row_tiles * p.col_tiles;
     const hipStream_t s = (hipStream_t)stream;
-    if (x_dtype == TS_ROW_BF16 && format == TS_FP8_E4M3) launch_quantize<uint16_t, TS_FP8_E4M3>(p, tiles, s);
-    else if (x_dtype == TS_ROW_BF16) launch_quantize<uint16_t, TS_FP8_E5M2>(p, tiles, s);
-    else if (format == TS_FP8_E4M3) launch_quantize<float, TS_FP8_E4M3>(p, tiles, s);
-    else launch_quantize<float, TS_FP8_E5M2>(p, tiles, s);
+    if (format == TS_FP8_E4M3) launch_quantize<TS_FP8_E4M3>(p, x_dtype == TS_ROW_BF16, s);
+    else launch_quantize<TS_FP8_E5M2>(p, x_dtype == TS_ROW_BF16, s);
     return hipGetLastError() == hipSuccess ? TS_OK : TS_ERR_HIP;
 }
 

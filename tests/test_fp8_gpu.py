@@ -392,3 +392,21 @@ def test_scales_at_the_ends(M, N, K, low, high):
         assert np.array_equal(got, torch.from_numpy(want).to(BF16).double().numpy())
     else:
         raise AssertionError("not a case")
+
+
+@pytest.mark.parametrize("rows,cols", [(2000, 8301), (1030, 16392), (4097, 4100)])
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+def test_quantize_many_tiles(rows, cols, dtype):
+    """An odd number of blocks to a row, rows that begin anywhere and end inside eight elements."""
+    x = values_of_many_sizes(rows, cols).to(dtype)
+    h = x.float().numpy()
+    q, s, qt, st = quantized(x, E4M3)
+    for codes, scales, of in ((q, s, h), (qt, st, h.T)):
+        want, want_scales = op.quantize(of, E4M3)
+        assert np.array_equal(scales.cpu().numpy(), want_scales)
+        same_codes(codes, want, E4M3)
+
+
+def values_of_many_sizes(rows, cols):
+    g = torch.Generator().manual_seed(cols)
+    return torch.randn(rows, cols, generator=g) * torch.exp2(torch.randn(rows, 1, generator=g) * 8)
