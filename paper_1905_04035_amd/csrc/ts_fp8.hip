@@ -511,13 +511,14 @@ __device__ __forceinline__ void wait_and_meet()
 {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER < 63 ? LATER : 63) : "memory");
 }
-// The same with LATER where the last accesses are stores behind the loads in question, else with none.  (In one statement: a branch would end the run of
+// The same with WITH_STORES where stores lie among the accesses behind the loads in question, else with LATER.  (In one statement: a branch would end the run of
 // instructions that keeps its order.)
-template <int LATER>
+template <int LATER, int WITH_STORES>
 __device__ __forceinline__ void meet_behind_stores(bool behind)
 {
-    asm volatile("s_cmp_lg_u32 %1, 0\n\ts_cbranch_scc1 .Lstores_%=\n\ts_waitcnt vmcnt(0)\n.Lstores_%=:\n\ts_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier"
-                 ::"n"(LATER < 63 ? LATER : 63), "s"(__builtin_amdgcn_readfirstlane((int)behind)) : "memory", "scc");
+    static_assert(LATER <= WITH_STORES, "the second wait adds nothing to the first");
+    asm volatile("s_cmp_lg_u32 %2, 0\n\ts_cbranch_scc1 .Lstores_%=\n\ts_waitcnt vmcnt(%0)\n.Lstores_%=:\n\ts_waitcnt vmcnt(%1) lgkmcnt(0)\n\ts_barrier"
+                 ::"n"(LATER < 63 ? LATER : 63), "n"(WITH_STORES < 63 ? WITH_STORES : 63), "s"(__builtin_amdgcn_readfirstlane((int)behind)) : "memory", "scc");
 }
 
 #ifdef __HIP_DEVICE_COMPILE__     // (a buffer's type is none of the host compiler's)
@@ -530,18 +531,18 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const uint8_t* p, int64
 }
 #endif
 
-// Sizes that the host needs, too.  LDS: two stages of [ROWS][128] codes, two of [ROWS] words of scales, 1 KiB that nobody reads, and eight rows of
+// Sizes that the host needs, too.  LDS: S stages (2 or 4) of [ROWS][128] codes, two of [ROWS] words of scales, 1 KiB that nobody reads, and eight rows of
 // the result for every wavefront.
-template <bool HALF, int WN, int WM, int NF, int MF>
+template <bool HALF, int WN, int WM, int NF, int MF, int S>
 struct Tile {
-    static constexpr int TN = 16 * WN * NF, TM = 16 * WM * MF, ROWS = TN + TM, STAGE = ROWS * kBlock, SCALES = 2 * STAGE, UNREAD = SCALES + 2 * ROWS * 4;
+    static constexpr int TN = 16 * WN * NF, TM = 16 * WM * MF, ROWS = TN + TM, STAGE = ROWS * kBlock, SCALES = S * STAGE, UNREAD = SCALES + 2 * ROWS * 4;
     static constexpr int EF = HALF ? NF : NF / 2, PITCH = EF * 16 * (HALF ? 2 : 4) + 16;       // fragments of a turn of the result; bytes of a row
     static constexpr int RESULT = UNREAD + 1024, LDS = RESULT + WN * WM * 8 * PITCH;
 };
 
 // A work-group of WN x WM wavefronts computes tiles of TN columns by TM rows of the result, a wavefront NF x MF fragments of 16 x 16, whose sums stay in
-// its registers; it takes tile after tile, as many work-groups as the GPU holds.  Codes go from memory into LDS past the registers, one block of 128
-// along K ahead.  Bound by the matrix instructions, the loads' latencies between them and, where K is short, by writing the result (256 x 256):
+// its registers; it takes tile after tile, as many work-groups as the GPU holds.  Codes go from memory into LDS past the registers, in S stages: up to S - 1
+// blocks of 128 along K ahead.  Bound by the matrix instructions, the loads' latencies between them and, where K is short, by writing the result (256 x 256):
 //                                       us       TFLOP/s    without any loads / without any accesses
 //   8192^3 to bf16                      401      2740       319 / 272 us
 //   8192 x 32768 x 1024 to bf16         283      1940       203 / 181, without stores 233
@@ -549,11 +550,11 @@ struct Tile {
 // What else was measured and lost: a ring of four half-blocks with 32 x 32 x 64 products (500 and 317 us: half lines of 64 bytes, twice the requests to L2),
 // 128 x 128 tiles everywhere (540 and 343), four wavefronts of 128 x 128 (431 and 302), work-groups that begin one after the other, so that not all
 // store at a time (8192^3 15 % slower).
-template <int FA, int FB, bool HALF, bool ONTO, int WN, int WM, int NF, int MF>
+template <int FA, int FB, bool HALF, bool ONTO, int WN, int WM, int NF, int MF, int S>
 __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel([[maybe_unused]] Matmul p)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-    typedef Tile<HALF, WN, WM, NF, MF> T;
+    typedef Tile<HALF, WN, WM, NF, MF, S> T;
     constexpr int TN = T::TN, TM = T::TM, ROWS = T::ROWS, STAGE = T::STAGE, SCALES = T::SCALES, WAVES = WN * WM;
     constexpr int LB = TN / (8 * WAVES), LA = TM / (8 * WAVES);     // loads of 1 KiB by a wavefront, for one block
     static_assert(TN % (8 * WAVES) == 0 && TM % (8 * WAVES) == 0 && TN % 64 == 0 && TM % 64 == 0, "whole loads");
@@ -606,7 +607,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel([[maybe_unused]] 
     constexpr int LS = (ROWS / 64 + WAVES - 1) / WAVES, LOADS = LB + LA + LS;
     const auto fetch = [&](int k, int j, bool wanted = true) {
         const bool there = wanted && k < blocks;
-        uint8_t* const to = wanted ? lds + (k & 1) * STAGE : nullptr;          // (a load that was made before: to where nobody looks)
+        uint8_t* const to = wanted ? lds + (k & (S - 1)) * STAGE : nullptr;          // (a load that was made before: to where nobody looks)
         uint8_t* const unread = lds + T::UNREAD;
         const int at_k = there ? k * kBlock : 0;            // (never more than a buffer's length)
         if (j < LB) {
@@ -651,13 +652,14 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel([[maybe_unused]] 
     constexpr int STORES = MF * (NF / EF) * (16 / TURN);
     // loads of the block after the next that are made before the next one begins
     constexpr int FIRST = !HALF ? 0 : NF / 2 * AT_ONCE < LOADS ? NF / 2 * AT_ONCE : LOADS;
+    constexpr int AHEAD_K = HALF ? S : S - 1;        // blocks that are asked for before the first is multiplied
     int64_t tile = blockIdx.x;
     turn_to(tile);
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) fetch(0, j);
+    for (int k = 0; k < AHEAD_K; ++k)
 #pragma unroll
-    for (int j = 0; j < (HALF ? LOADS : 0); ++j) fetch(1, j);
-    wait_and_meet<HALF ? LOADS : 0>();
+        for (int j = 0; j < LOADS; ++j) fetch(k, j);
+    wait_and_meet<(AHEAD_K - 1) * LOADS>();
     bool behind = false;        // stores of the last tile lie between the loads
     for (;;) {
         f4 acc[NF][MF];
@@ -675,7 +677,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel([[maybe_unused]] 
             for (int h = 0; h < MF; ++h) widen<FA>(v[h], sa[h] & 255u, wide[h]);
         }
         for (int k = 0; k < blocks; ++k) {
-            const int stage = (k & 1) * STAGE, next = STAGE - stage;
+            const int stage = (k & (S - 1)) * STAGE, next = ((k + 1) & (S - 1)) * STAGE;
             if constexpr (HALF) {
                 // First half of the fragments of B: each is multiplied while the one after it is read, and the second half's are read besides.
                 constexpr int H = NF / 2;
@@ -688,7 +690,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel([[maybe_unused]] 
                     keep_order();
 #pragma unroll
                     for (int j = (H + f) * AT_ONCE; j < (H + f + 1) * AT_ONCE; ++j)
-                        if (j < LOADS) fetch(k + 1, j, k > 0);
+                        if (j < LOADS) fetch(k + S - 1, j, k > 0);
 #pragma unroll
                     for (int h = 0; h < MF; ++h)
                         acc[f][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v[h], acc[f][h], FB, FA, 0, (int)sb[f], 0, (int)sa[h]);
@@ -696,14 +698,14 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel([[maybe_unused]] 
                     u = un;
                 }
                 // All of this stage is in registers: it is given back.  Second half: as soon as a fragment of A is done with, the next block's is read.
-                meet_behind_stores<STORES + LOADS - FIRST>(behind && k == 0);
+                meet_behind_stores<(S - 2) * LOADS, (S - 2) * LOADS + STORES + LOADS - FIRST>(behind && k == 0);
                 u = codes_b(next, 0);
 #pragma unroll
                 for (int h = 0; h < MF; ++h) {
                     keep_order();
 #pragma unroll
                     for (int j = h * H * AT_ONCE / MF; j < (h + 1) * H * AT_ONCE / MF; ++j)
-                        if (j < LOADS) fetch(k + 2, j);
+                        if (j < LOADS) fetch(k + S, j);
 #pragma unroll
                     for (int f = 0; f < H; ++f)
                         acc[H + f][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[f], v[h], acc[H + f][h], FB, FA, 0, (int)sb[H + f], 0, (int)sa[h]);
@@ -713,12 +715,12 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel([[maybe_unused]] 
             } else {
 #pragma unroll
                 for (int f = 0; f < NF; ++f) {
-                    if (f + 1 == NF) wait_and_meet();
+                    if (f + 1 == NF) wait_and_meet<(S - 2) * LOADS>();
                     const i8 un = f + 1 < NF ? codes_b(stage, f + 1) : codes_b(next, 0);
                     keep_order();
 #pragma unroll
                     for (int j = f * AT_ONCE; j < (f + 1) * AT_ONCE; ++j)
-                        if (j < LOADS) fetch(k + 1, j);
+                        if (j < LOADS) fetch(k + S - 1, j);
                     b8 x[4];
                     widen<FB>(u, sb[f] & 255u, x);
 #pragma unroll
@@ -762,9 +764,9 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel([[maybe_unused]] 
         if (tile < all) {
             turn_to(tile);
 #pragma unroll
-            for (int j = 0; j < LOADS; ++j) fetch(0, j);
+            for (int k = 0; k < AHEAD_K; ++k)
 #pragma unroll
-            for (int j = 0; j < (HALF ? LOADS : 0); ++j) fetch(1, j);
+                for (int j = 0; j < LOADS; ++j) fetch(k, j);
         }
         if (in_parts) {
             f4* const to = p.sums + ((done - p.full) * WAVES + wave) * (NF * MF * 64) + lane;
@@ -841,17 +843,17 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel([[maybe_unused]] 
         if (tile >= all) return;
         // the loads are older than the stores: where every store was made, these may still be on their way
         behind = whole;
-        if (whole) wait_and_meet<(HALF ? LOADS : 0) + STORES>();
+        if (whole) wait_and_meet<(AHEAD_K - 1) * LOADS + STORES>();
         else wait_and_meet();
     }
 #endif
 }
 
 // The tiles that were computed in parts: their sums, in the parts' order, and c_in.  A work-group takes one fragment of each wavefront of a tile.
-template <bool HALF, int WN, int WM, int NF, int MF>
+template <bool HALF, int WN, int WM, int NF, int MF, int S>
 __global__ __launch_bounds__(64 * WN * WM) void parts_kernel(Matmul p)
 {
-    typedef Tile<HALF, WN, WM, NF, MF> T;
+    typedef Tile<HALF, WN, WM, NF, MF, S> T;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wn = wave % WN, wm = wave / WN, i = lane & 15, g = lane >> 4;
     const int64_t rest = p.m_tiles * p.n_tiles - p.full, t = blockIdx.x / (NF * MF);
     const int fh = (int)(blockIdx.x % (NF * MF)), f = fh / MF, h = fh - f * MF;
@@ -918,7 +920,7 @@ void launch_quantize(const Quantize& p, bool half, hipStream_t stream)
 
 // How a product is computed.  The form and the number of parts fix the order of additions, so they follow from the sizes and the result's type alone,
 // as if for a GPU of 256 compute units.
-enum { FORM_ROWS, FORM_LOW, FORM_SMALL, FORM_LARGE };
+enum { FORM_ROWS, FORM_LOW, FORM_DEEP, FORM_SMALL, FORM_LARGE };
 struct Way {
     int form;
     int parts, part_blocks;
@@ -935,6 +937,7 @@ struct Form {
 };
 constexpr Form kForms[] = {{0, 0, 0, {0, 0}, {0, 0}, 0},
                            {64, 128, 2, {1.10, 0.80}, {4.0, 2.5}, 2.5},
+                           {64, 128, 1, {0.75, 0.33}, {3.5, 2.2}, 2.0},       // four stages
                            {128, 128, 2, {1.70, 1.15}, {6.0, 3.0}, 3.0},
                            {256, 256, 1, {2.75, 1.55}, {14.0, 6.0}, 6.0}};
 constexpr int kUnits = 256;
@@ -946,6 +949,8 @@ double rounds_us(const Form& c, int64_t wgs, double each)
     return whole * each + (per_unit % c.beside ? 0.7 * each : 0.0);
 }
 
+// A work-group that has a compute unit to itself waits for its loads with two stages; with four it does not, 64 x 128 1239 x 1024 x 3419 to bf16 13.3 us / 20.3, 7135
+// x 104 x 15275 30.1 / 36.9, 562 x 80 x 39483 to fp32 19.0 / 21.5.  Two beside each other hide their waits as well: four stages, which leave room for one, lose there.
 // What was measured (us) / what one tile size for all would take, without parts: 33801 x 1024 x 4987 to fp32 269 / 322 (256 x 256: its third round has 20 tiles), 300 x 1024 x 20000
 // to fp32 29 / 366, 1000 x 512 x 8000 to bf16 18 / 75, 12000 x 500 x 4000 to fp32 59 / 86, 8192 x 1024 x 32768 to fp32 391 (256 x 256 in two parts) / 477 (128 x 128).
 Way way_for(int64_t M, int64_t N, int64_t K, bool half)
@@ -986,18 +991,18 @@ Way way_for(int64_t M, int64_t N, int64_t K, bool half)
 
 int64_t parts_bytes(const Way& w) { return w.parts > 1 ? w.rest * w.parts * kForms[w.form].tm * kForms[w.form].tn * 4 : 0; }
 
-template <int FA, int FB, bool HALF, int WN, int WM, int NF, int MF>
+template <int FA, int FB, bool HALF, int WN, int WM, int NF, int MF, int S>
 void launch_tiles(Matmul p, hipStream_t stream)
 {
-    typedef Tile<HALF, WN, WM, NF, MF> T;
+    typedef Tile<HALF, WN, WM, NF, MF, S> T;
     p.n_tiles = (p.N + T::TN - 1) / T::TN;
     p.m_tiles = (p.M + T::TM - 1) / T::TM;
-    const auto kernel = !HALF && p.c_in ? tile_kernel<FA, FB, HALF, !HALF, WN, WM, NF, MF> : tile_kernel<FA, FB, HALF, false, WN, WM, NF, MF>;
+    const auto kernel = !HALF && p.c_in ? tile_kernel<FA, FB, HALF, !HALF, WN, WM, NF, MF, S> : tile_kernel<FA, FB, HALF, false, WN, WM, NF, MF, S>;
     const int lds = T::LDS;
     const int64_t rest = p.m_tiles * p.n_tiles - p.full, all = p.full + rest * p.parts;
     const int64_t most = (int64_t)compute_units() * (160 * 1024 / lds);          // as many work-groups as there is room for
     hipLaunchKernelGGL(kernel, dim3((unsigned)(all < most ? all : most)), dim3(64 * WN * WM), lds, stream, p);
-    if (p.parts > 1) hipLaunchKernelGGL((parts_kernel<HALF, WN, WM, NF, MF>), dim3((unsigned)(rest * NF * MF)), dim3(64 * WN * WM), 0, stream, p);
+    if (p.parts > 1) hipLaunchKernelGGL((parts_kernel<HALF, WN, WM, NF, MF, S>), dim3((unsigned)(rest * NF * MF)), dim3(64 * WN * WM), 0, stream, p);
 }
 
 template <int FA, int FB, bool HALF, int MF>
@@ -1014,9 +1019,10 @@ void launch_rows(Matmul p, int log_kw, hipStream_t stream)
 template <int FA, int FB, bool HALF>
 void launch_matmul(const Matmul& p, const Way& w, hipStream_t stream)
 {
-    if (w.form == FORM_LARGE) launch_tiles<FA, FB, HALF, 2, 4, 8, 4>(p, stream);
-    else if (w.form == FORM_SMALL) launch_tiles<FA, FB, HALF, 2, 2, 4, 4>(p, stream);
-    else if (w.form == FORM_LOW) launch_tiles<FA, FB, HALF, 2, 2, 4, 2>(p, stream);
+    if (w.form == FORM_LARGE) launch_tiles<FA, FB, HALF, 2, 4, 8, 4, 2>(p, stream);
+    else if (w.form == FORM_SMALL) launch_tiles<FA, FB, HALF, 2, 2, 4, 4, 2>(p, stream);
+    else if (w.form == FORM_LOW) launch_tiles<FA, FB, HALF, 2, 2, 4, 2, 2>(p, stream);
+    else if (w.form == FORM_DEEP) launch_tiles<FA, FB, HALF, 2, 2, 4, 2, 4>(p, stream);
     else if (p.M <= 16) launch_rows<FA, FB, HALF, 1>(p, w.log_kw, stream);
     else launch_rows<FA, FB, HALF, 2>(p, w.log_kw, stream);
 }

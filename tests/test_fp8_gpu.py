@@ -287,7 +287,8 @@ def test_shapes_and_types_of_the_binding():
 
 
 # large and small tiles, several to a work-group, tiles that end inside, unfinished rounds in parts: sizes at which each is taken
-@pytest.mark.parametrize("M,N,K", [(4096, 4096, 1024), (8500, 2100, 5000), (2000, 9001, 300), (1500, 1500, 3000), (8192, 1024, 6000), (600, 8000, 128)])
+@pytest.mark.parametrize("M,N,K", [(4096, 4096, 1024), (8500, 2100, 5000), (2000, 9001, 300), (1500, 1500, 3000), (8192, 1024, 6000), (600, 8000, 128),
+                                   (1239, 1024, 3419), (280, 181, 20000), (1280, 1920, 4000), (4000, 700, 1000), (100, 130, 520)])
 @pytest.mark.parametrize("kind", ["bf16", "fp32", "onto", "in place"])
 def test_large_products_of_whole_numbers_are_exact(M, N, K, kind):
     a, sa = operand(M, K, E4M3, "whole", M + K)
