@@ -117,8 +117,7 @@ struct Quantize {
     int64_t row_tiles, col_tiles;
 };
 
-// Eight rows of eight elements as they lie in memory, at any address that is aligned to one, zeros beyond the matrix (WHOLE: a row's length is a multiple of eight);
-// and the bits of the largest magnitudes of a row and of all columns,
+// Eight rows of eight elements as they lie in memory, at any address that is aligned to one; and the bits of the largest magnitudes of a row and of all columns,
 // which show whether a value is no finite number.
 template <typename T>
 struct Part;
@@ -127,20 +126,14 @@ template <>
 struct Part<float> {
     f4 v[8][2];
 
-    template <bool WHOLE>
-    __device__ __forceinline__ void load(int i, const float* p, int64_t left)
+    __device__ __forceinline__ void clear(int i) { v[i][0] = v[i][1] = (f4)(0.0f); }
+    __device__ __forceinline__ void load(int i, const float* p)
     {
         typedef f4 __attribute__((aligned(4))) any_f4;
-        v[i][0] = v[i][1] = (f4)(0.0f);
-        if (left >= 8) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) v[i][h] = __builtin_nontemporal_load(reinterpret_cast<const any_f4*>(p) + h);
-        } else if (!WHOLE) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < left) v[i][j >> 2][j & 3] = p[j];
-        }
+        for (int h = 0; h < 2; ++h) v[i][h] = __builtin_nontemporal_load(reinterpret_cast<const any_f4*>(p) + h);
     }
+    __device__ __forceinline__ void set(int i, int c, float x) { v[i][c >> 2][c & 3] = x; }
     __device__ __forceinline__ float value(int i, int c) const { return v[i][c >> 2][c & 3]; }
     __device__ __forceinline__ f4 four(int i, int h) const { return v[i][h]; }
     // (two magnitudes in one instruction; a quiet NaN is passed over, as it should be)
@@ -173,19 +166,13 @@ struct Part<uint16_t> {
     typedef uint16_t h2 __attribute__((ext_vector_type(2)));
     u4 v[8];
 
-    template <bool WHOLE>
-    __device__ __forceinline__ void load(int i, const uint16_t* p, int64_t left)
+    __device__ __forceinline__ void clear(int i) { v[i] = (u4)(0u); }
+    __device__ __forceinline__ void load(int i, const uint16_t* p)
     {
         typedef u4 __attribute__((aligned(2))) any_u4;
-        v[i] = (u4)(0u);
-        if (left >= 8) {
-            v[i] = __builtin_nontemporal_load(reinterpret_cast<const any_u4*>(p));
-        } else if (!WHOLE) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < left) v[i][j >> 1] |= (uint32_t)p[j] << (j & 1) * 16;
-        }
+        v[i] = __builtin_nontemporal_load(reinterpret_cast<const any_u4*>(p));
     }
+    __device__ __forceinline__ void set(int i, int c, uint16_t x) { v[i][c >> 1] = c & 1 ? v[i][c >> 1] | (uint32_t)x << 16 : x; }
     __device__ __forceinline__ float value(int i, int c) const { return __uint_as_float(c & 1 ? v[i][c >> 1] & 0xFFFF0000u : v[i][c >> 1] << 16); }
     __device__ __forceinline__ f4 four(int i, int h) const { return f4{value(i, 4 * h), value(i, 4 * h + 1), value(i, 4 * h + 2), value(i, 4 * h + 3)}; }
     // (two magnitudes in one instruction, as 16-bit numbers)
@@ -224,8 +211,9 @@ __device__ __forceinline__ uint32_t finite_size(float x)
 // looked at again without them.  Bound by memory, and so by how many tiles a compute unit holds: bf16 elements stay as they are, two to a register.
 // 8192 x 32768 bf16 to e5m2, both ways / rows only: 203 us = 5.3 TB/s / 142 = 5.7 (261 / 181 with fp32 in the registers and every magnitude by itself).
 // Two tiles, whose stretches are twice as long, against one: 205 / 210 us there, 8320 x 33152 219 / 234; against two below each other 205 / 212 and 219 / 226.
+// Wavefronts to a SIMD: five of bf16, four of fp32, of which a fifth one makes more requests than memory takes well (8192 x 32768 rows only 273 us, so 281).
 template <typename T, int FMT, bool WHOLE, int WIDE>
-__global__ __launch_bounds__(256 * WIDE, sizeof(T) == 2 ? 5 : 4) void quantize_kernel(Quantize p)
+__global__ __launch_bounds__(256 * WIDE) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 5 : 4, sizeof(T) == 2 ? 5 : 4))) void quantize_kernel(Quantize p)
 {
     __shared__ __align__(16) uint32_t most_of[4 * WIDE][WIDE * kBlock];
     __shared__ __align__(16) uint8_t turned[WIDE * kBlock][kBlock + 8];
@@ -238,8 +226,26 @@ __global__ __launch_bounds__(256 * WIDE, sizeof(T) == 2 ? 5 : 4) void quantize_k
     const int64_t c_tile = c_wide * WIDE + c8 / kBlock;
     const bool here = WIDE == 1 || c_tile < p.col_tiles;
     Part<T> x;
+    const int64_t left = here ? p.cols - c0 : 0, below = p.rows - r0;
+    const T* const from = (const T*)p.x + r0 * p.cols + c0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x.template load<WHOLE>(i, (const T*)p.x + (r0 + i) * p.cols + c0, r0 + i < p.rows && here ? p.cols - c0 : 0);
+    for (int i = 0; i < 8; ++i) {
+        x.clear(i);
+        if (left >= 8 && i < below) x.load(i, from + i * p.cols);
+    }
+    // A row's end inside eight elements: one by one, all of them asked for before one is looked at (7118 x 948 bf16 rows only 6.7 us, one
+    // row's after the other 12.3).
+    if (!WHOLE && left > 0 && left < 8 && below > 0) {
+        T e[8][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) e[i][c] = from[(i < below ? i : 0) * p.cols + (c < left ? c : 0)];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) x.set(i, c, i < below && c < left ? e[i][c] : T(0));
+    }
     if (p.q) {
         const int64_t ld = code_row(p.cols), lds = scale_row(p.cols);
 #pragma unroll
