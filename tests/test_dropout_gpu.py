@@ -1,5 +1,5 @@
 """Dropout with a mask that is never stored, the lookup in front of it and the densify behind it, on the GPU against the
-checker.  Tolerances count roundings: half a step is 2^-24 (fp32) or 2^-8 (bf16) of the value."""
+oracle.  Tolerances count roundings: half a step is 2^-24 (fp32) or 2^-8 (bf16) of the value."""
 import numpy as np
 import pytest
 import torch

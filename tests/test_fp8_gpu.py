@@ -1,4 +1,4 @@
-"""8-bit codes with a scale for each block of 128, and products of them, on the GPU against the checker.
+"""8-bit codes with a scale for each block of 128, and products of them, on the GPU against the oracle.
 
 Codes and scales are compared bit for bit.  Products of two codes have at most 8 significant bits and are exact in fp32, so an
 element's error comes from its additions alone: at most K rounded ones (and the c_in), each off by at most 2^-23 of

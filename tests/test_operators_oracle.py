@@ -1,4 +1,4 @@
-"""What pins the checker of dropout, lookup and 8-bit products (no GPU)."""
+"""What pins the oracle of dropout, lookup and 8-bit products (no GPU)."""
 import numpy as np
 import pytest
 import torch
