@@ -434,37 +434,45 @@ __device__ __forceinline__ i8 load_codes(const uint8_t* p)
 }
 
 // ---- few rows: codes straight into registers
-// A wavefront computes 16 columns of the result in MF * 16 rows: lane l holds 32 codes of row l % 16 of a fragment.  It takes every kw-th run of four
+// A wavefront computes 16 * NF columns of the result in MF * 16 rows: lane l holds 32 codes of row l % 16 of a fragment.  It takes every kw-th run of four
 // blocks, all of whose codes it asks for at once; the kw wavefronts of one place add their sums up in LDS, in their order.  Bound by reading B once:
-// one row, N = 32768, K = 1024 6.9 us = 4.9 TB/s, a launch of 2 us included; sixteen rows to bf16 9.4.
-template <int FA, int FB, bool HALF, int MF>
+// one row, N = 32768, K = 1024 6.9 us = 4.9 TB/s, a launch of 2 us included; and, with more rows, by the L1 caches: neighbouring lanes' codes lie in different
+// rows and so in different lines.
+template <int FA, int FB, bool HALF, int MF, int NF>
 __global__ __launch_bounds__(256) void rows_kernel(Matmul p, int log_kw)
 {
-    __shared__ f4 sums[4][MF][64];
+    __shared__ f4 sums[4][NF * MF][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const int kw = 1 << log_kw, part = wave & (kw - 1), places = (int)(blockDim.x >> 6) >> log_kw;
-    const int64_t n0 = p.n_first + ((int64_t)blockIdx.x * places + (wave >> log_kw)) * 16;
-    const int64_t n = n0 + i, rb = n < p.N ? n : p.N - 1;                 // rows past the end: the last one again
-    const uint8_t *const b = p.b + rb * p.ld + g * 32, *const sb = p.b_scales + rb * p.lds;
-    const uint8_t *a[MF], *sa[MF];
-    f4 acc[MF];
+    const int64_t n0 = p.n_first + ((int64_t)blockIdx.x * places + (wave >> log_kw)) * (16 * NF);
+    const uint8_t *b[NF], *sb[NF], *a[MF], *sa[MF];
+    f4 acc[NF][MF];
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+        const int64_t n = n0 + f * 16 + i, rb = n < p.N ? n : p.N - 1;                 // rows past the end: the last one again
+        b[f] = p.b + rb * p.ld + g * 32;
+        sb[f] = p.b_scales + rb * p.lds;
+    }
 #pragma unroll
     for (int h = 0; h < MF; ++h) {
         const int64_t m = h * 16 + i, ra = m < p.M ? m : p.M - 1;
         a[h] = p.a + ra * p.ld + g * 32;
         sa[h] = p.a_scales + ra * p.lds;
-        acc[h] = (f4)(0.0f);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) acc[f][h] = (f4)(0.0f);
     }
     for (int k = part * 4; k < p.blocks; k += kw * 4) {
-        const uint32_t wb = *reinterpret_cast<const uint32_t*>(sb + k);
-        uint32_t wa[MF];
+        uint32_t wb[NF], wa[MF];
+#pragma unroll
+        for (int f = 0; f < NF; ++f) wb[f] = *reinterpret_cast<const uint32_t*>(sb[f] + k);
 #pragma unroll
         for (int h = 0; h < MF; ++h) wa[h] = *reinterpret_cast<const uint32_t*>(sa[h] + k);
-        i8 u[4], v[4][MF];
+        i8 u[4][NF], v[4][MF];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int64_t at = (int64_t)(k + q < p.blocks ? k + q : p.blocks - 1) * kBlock;      // (behind the last block: it again, unused)
-            u[q] = load_codes(b + at);
+#pragma unroll
+            for (int f = 0; f < NF; ++f) u[q][f] = load_codes(b[f] + at);
 #pragma unroll
             for (int h = 0; h < MF; ++h) v[q][h] = load_codes(a[h] + at);
         }
@@ -473,17 +481,22 @@ __global__ __launch_bounds__(256) void rows_kernel(Matmul p, int log_kw)
             if (k + q >= p.blocks) break;
             if constexpr (HALF) {
 #pragma unroll
-                for (int h = 0; h < MF; ++h)
-                    acc[h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u[q], v[q][h], acc[h], FB, FA, 0, (int)(wb >> 8 * q), 0, (int)(wa[h] >> 8 * q));
+                for (int f = 0; f < NF; ++f)
+#pragma unroll
+                    for (int h = 0; h < MF; ++h)
+                        acc[f][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u[q][f], v[q][h], acc[f][h], FB, FA, 0, (int)(wb[f] >> 8 * q), 0, (int)(wa[h] >> 8 * q));
             } else {
-                b8 x[4];
-                widen<FB>(u[q], (wb >> 8 * q) & 255u, x);
+                b8 x[NF][4];
+#pragma unroll
+                for (int f = 0; f < NF; ++f) widen<FB>(u[q][f], (wb[f] >> 8 * q) & 255u, x[f]);
 #pragma unroll
                 for (int h = 0; h < MF; ++h) {
                     b8 y[4];
                     widen<FA>(v[q][h], (wa[h] >> 8 * q) & 255u, y);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[r], y[r], acc[h], 0, 0, 0);
+                    for (int f = 0; f < NF; ++f)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[f][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[f][r], y[r], acc[f][h], 0, 0, 0);
                 }
             }
         }
@@ -491,20 +504,25 @@ __global__ __launch_bounds__(256) void rows_kernel(Matmul p, int log_kw)
     if (kw > 1) {
         if (part > 0) {
 #pragma unroll
-            for (int h = 0; h < MF; ++h) sums[wave][h][lane] = acc[h];
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                for (int h = 0; h < MF; ++h) sums[wave][f * MF + h][lane] = acc[f][h];
         }
         __syncthreads();
         if (part > 0) return;
         for (int w = 1; w < kw; ++w)
 #pragma unroll
-            for (int h = 0; h < MF; ++h) acc[h] += sums[wave + w][h][lane];
-    }
-    const int64_t n4 = n0 + g * 4;
+            for (int f = 0; f < NF; ++f)
 #pragma unroll
-    for (int h = 0; h < MF; ++h) {
-        const int64_t m = h * 16 + i;
-        if (m < p.M) store4<HALF>(p, m, n4, acc[h]);
+                for (int h = 0; h < MF; ++h) acc[f][h] += sums[wave + w][f * MF + h][lane];
     }
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int h = 0; h < MF; ++h) {
+            const int64_t m = h * 16 + i;
+            if (m < p.M) store4<HALF>(p, m, n0 + f * 16 + g * 4, acc[f][h]);
+        }
 }
 
 // ---- large products: tiles through LDS
@@ -932,6 +950,7 @@ struct Way {
     int parts, part_blocks;
     int64_t full, rest;     // tiles that are computed whole, and in parts
     int log_kw;             // FORM_ROWS: wavefronts that share a place
+    bool two;               // FORM_ROWS: places of 32 columns
 };
 
 // A form's tiles, how many of them a compute unit computes at a time, and the microseconds that these take: per block of 128 along K (half / full: for a
@@ -962,12 +981,16 @@ double rounds_us(const Form& c, int64_t wgs, double each)
 Way way_for(int64_t M, int64_t N, int64_t K, bool half)
 {
     const int blocks = (int)(code_row(K) / kBlock);
-    Way w{FORM_ROWS, 1, blocks, 0, 0, 0};
+    Way w{FORM_ROWS, 1, blocks, 0, 0, 0, false};
     // Up to 32 rows the matrix instructions are idle anyway: B is read past LDS.  One wavefront has work for its latencies with eight blocks; where there are
     // few places, up to four share one.  32 x 7003 x 512 to bf16 4.4 us, in tiles 5.6; 33 x 32768 x 1024 in tiles 10.4, in three fragments 13.
     if (M <= 32) {
         const int64_t places = (N + 15) / 16;
         while (w.log_kw < 2 && (places << w.log_kw) < 2048 && (4 << w.log_kw) < blocks) ++w.log_kw;
+        // Places of 32 columns ask for A's codes half as often, where there are wavefronts enough and that is much of the work, us with 32 / 16: 32 x 32768 x 1024
+        // to bf16 11.2 / 13.3, to fp32 10.1 / 13.4, 16 rows 9.1 / 9.5 and 8.1 / 9.6, one 8.3 / 6.8 and 7.1 / 7.0; 8192 x 4096, one row 9.1 / 10.4 and 8.7 /
+        // 10.5; 10000 x 512, 32 rows 6.1 / 4.8.
+        w.two = (places << w.log_kw) >= 1500 && (M > 16 || blocks >= 32 || (!half && M > 1 && blocks >= 8));
         return w;
     }
     double best = 1e30;
@@ -979,7 +1002,7 @@ Way way_for(int64_t M, int64_t N, int64_t K, bool half)
         const double us = rounds_us(c, tiles, whole);
         if (us < best) {
             best = us;
-            w = Way{form, 1, blocks, tiles, 0, 0};
+            w = Way{form, 1, blocks, tiles, 0, 0, false};
         }
         const int64_t rest = tiles % room ? tiles % room : tiles == room ? room : 0;
         for (int parts = 2; rest > 0 && parts <= 64 && parts * 4 <= blocks + 3; ++parts) {
@@ -988,7 +1011,7 @@ Way way_for(int64_t M, int64_t N, int64_t K, bool half)
             const double us = rounds_us(c, tiles - rest, whole) + rounds_us(c, rest * parts, per * block + c.part) + 3 + (double)(rest * c.tm * c.tn) * (4 * parts + 4) / 4e6;
             if (us < best) {
                 best = us;
-                w = Way{form, parts, per, tiles - rest, rest, 0};
+                w = Way{form, parts, per, tiles - rest, rest, 0, false};
             }
         }
     }
@@ -1011,14 +1034,14 @@ void launch_tiles(Matmul p, hipStream_t stream)
     if (p.parts > 1) hipLaunchKernelGGL((parts_kernel<HALF, WN, WM, NF, MF, S>), dim3((unsigned)(rest * NF * MF)), dim3(64 * WN * WM), 0, stream, p);
 }
 
-template <int FA, int FB, bool HALF, int MF>
+template <int FA, int FB, bool HALF, int MF, int NF>
 void launch_rows(Matmul p, int log_kw, hipStream_t stream)
 {
     constexpr int waves = 4;
-    const int places = waves >> log_kw;
-    in_launches((p.N + 16 * places - 1) / (16 * places), kMaxWgs / 2, [&](int64_t at, unsigned n) {
-        p.n_first = at * 16 * places;
-        hipLaunchKernelGGL((rows_kernel<FA, FB, HALF, MF>), dim3(n), dim3(64 * waves), 0, stream, p, log_kw);
+    const int columns = 16 * NF * (waves >> log_kw);
+    in_launches((p.N + columns - 1) / columns, kMaxWgs / 2, [&](int64_t at, unsigned n) {
+        p.n_first = at * columns;
+        hipLaunchKernelGGL((rows_kernel<FA, FB, HALF, MF, NF>), dim3(n), dim3(64 * waves), 0, stream, p, log_kw);
     });
 }
 
@@ -1029,8 +1052,10 @@ void launch_matmul(const Matmul& p, const Way& w, hipStream_t stream)
     else if (w.form == FORM_SMALL) launch_tiles<FA, FB, HALF, 2, 2, 4, 4, 2>(p, stream);
     else if (w.form == FORM_LOW) launch_tiles<FA, FB, HALF, 2, 2, 4, 2, 2>(p, stream);
     else if (w.form == FORM_DEEP) launch_tiles<FA, FB, HALF, 2, 2, 4, 2, 4>(p, stream);
-    else if (p.M <= 16) launch_rows<FA, FB, HALF, 1>(p, w.log_kw, stream);
-    else launch_rows<FA, FB, HALF, 2>(p, w.log_kw, stream);
+    else if (p.M <= 16 && !w.two) launch_rows<FA, FB, HALF, 1, 1>(p, w.log_kw, stream);
+    else if (p.M <= 16) launch_rows<FA, FB, HALF, 1, 2>(p, w.log_kw, stream);
+    else if (!w.two) launch_rows<FA, FB, HALF, 2, 1>(p, w.log_kw, stream);
+    else launch_rows<FA, FB, HALF, 2, 2>(p, w.log_kw, stream);
 }
 
 template <int FA, int FB>

@@ -134,7 +134,8 @@ def product(a, sa, fa, b, sb, fb, K, dtype, c_in=None, in_place=False):
 # few rows, few columns, odd ones, tiles that end inside, one block and many, products that are split along K
 PRODUCTS = [(1, 1, 1), (1, 32768, 64), (1, 1000, 1024), (2, 130, 200), (7, 999, 300), (16, 512, 512), (17, 1001, 129), (33, 260, 4987),
             (64, 1024, 8192), (100, 100, 100), (128, 128, 128), (129, 257, 385), (256, 512, 640), (257, 255, 1000), (300, 5000, 64),
-            (1000, 64, 2048), (1024, 1024, 1024), (2000, 1500, 257), (515, 4097, 512), (1, 16, 40000), (40, 48, 70000)]
+            (1000, 64, 2048), (1024, 1024, 1024), (2000, 1500, 257), (515, 4097, 512), (1, 16, 40000), (40, 48, 70000),
+            (1, 8200, 4200), (16, 25003, 1024), (23, 24010, 300), (32, 8190, 1100)]
 
 
 @pytest.mark.parametrize("M,N,K", PRODUCTS)
