@@ -136,10 +136,11 @@ struct Part<float> {
     __device__ __forceinline__ void set(int i, int c, float x) { v[i][c >> 2][c & 3] = x; }
     __device__ __forceinline__ float value(int i, int c) const { return v[i][c >> 2][c & 3]; }
     __device__ __forceinline__ f4 four(int i, int h) const { return v[i][h]; }
-    // (two magnitudes in one instruction; a quiet NaN is passed over, as it should be)
+    // (two magnitudes in one instruction, of which any NaN makes a NaN, whose bits lie above all numbers'; v_max3_f32 passes over a signalling NaN
+    // together with the value beside it)
     static __device__ __forceinline__ float larger3(float most, float a, float b)
     {
-        asm("v_max3_f32 %0, |%1|, |%2|, %3" : "=v"(most) : "v"(a), "v"(b), "v"(most));
+        asm("v_maximum3_f32 %0, |%1|, |%2|, %3" : "=v"(most) : "v"(a), "v"(b), "v"(most));
         return most;
     }
     __device__ __forceinline__ uint32_t row_size(int i) const
