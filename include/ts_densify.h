@@ -242,7 +242,7 @@ int ts_quantize_fp8(const void* x, int32_t x_dtype, int64_t rows, int64_t cols, 
  * out[m, n] = c_in[m, n] + sum over k of A[m, k] B[n, k],  m < M, n < N, k < K
  *
  * a, a_scales: A [M, K]; b, b_scales: B [N, K]; formats TS_FP8_*, one for each; a scale byte of 255 stands for NaN.
- * Sums are fp32, in an order that follows from M, N and K alone: the same inputs give the same bits on every run.  out
+ * Sums are fp32, in an order that follows from M, N, K and out_dtype alone: the same inputs give the same bits on every run.  out
  * [M, N] is TS_OUT_FP32, made from exact products, or TS_OUT_BF16, made by the 8-bit matrix instructions, which cut what a
  * product has more than 13 bits below the largest of its group of eight along K (1.5e-5 of the result's norm on normal
  * data), and rounded once; c_in must be NULL with TS_OUT_BF16, else TS_ERR_SHAPE.  c_in fp32 [M, N] or NULL; it may be

@@ -5,7 +5,8 @@
 // 32-bit words goes through rounds of two 32 x 32 -> 64 bit products; any element's bits follow from its place and the key
 // alone, so nothing is stored and no order of evaluation matters.  Seven rounds: the fewest that pass the whole BigCrush
 // battery according to that paper (ten is its margin).  A round costs a lane two wide products, each four times as long as
-// an addition, per four elements; ten rounds would take 1.4 times as long where the products bound a kernel.
+// an addition, per four elements (thirteen in all: one of the first round's is the same for all lanes); ten rounds would take 1.5
+// times as long where the products bound a kernel.
 #ifndef TS_PHILOX_H
 #define TS_PHILOX_H
 
@@ -32,7 +33,7 @@ struct Mask {
 };
 
 // One instruction, which the compiler does not form by itself (two exclusive ors take
-// the dropout of 65536 x 1024 bf16 with a residual from 66.5 to 67.5 us, and ts_densify_dropout of 131072 x 1024 bf16 from 129 to 137).
+// the dropout of 65536 x 1024 bf16 with a residual from 66.4 to 67.3 us, and ts_densify_dropout of 131072 x 1024 bf16 from 121.6 to 128.1).
 __device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
 
 // Words of elements 4 * group .. 4 * group + 3.

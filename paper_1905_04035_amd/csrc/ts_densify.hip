@@ -265,8 +265,8 @@ __device__ __forceinline__ uint64_t drop_offset(const Drop& p)
 // The mask's share of a lane's columns col .. col + 4 * NV - 1 of the value row at row_addr: the place of four elements among the
 // call's follows from their address.
 // The sums' order is the one without a mask, and dropped elements are added as zeros: the mask costs arithmetic and no traffic.  Without / with it,
-// p = 0.1: 16384 fp32 rows of 1024, V = 32768 58.5 / 59.3 us; 60000 of them 101.7 / 108.4; 131072 bf16 rows 104.6 / 123.4, where 14 wide products
-// per four elements take as long as their eight bytes.
+// p = 0.1: 16384 fp32 rows of 1024, V = 32768 58.5 / 59.3 us; 60000 of them 101.7 / 108.4; 131072 bf16 rows 104.6 / 121.6, where thirteen wide
+// products per four elements take as long as their eight bytes.
 template <typename RowT, int EPI, int NV>
 __device__ __forceinline__ void drop_rows(f4 (&r)[NV], uint64_t row_addr, int col, uint64_t offset, const Drop& p)
 {
@@ -1250,7 +1250,7 @@ __device__ __forceinline__ void short_row(const ReduceParams& p, int v, int c0, 
     const bool copy = p.copy_untouched && v >= p.copy_row0;    // what to do if the row received no pair
     const bool early = copy;                                   // then only a long row makes the early load useless
     // value rows in flight together (16 KiB; 8 KiB measured 2 % slower where short rows have up to 32 pairs; with a mask the registers of eight rows
-    // leave room for fewer wavefronts, which then hide less of the mask's arithmetic: 131072 bf16 rows of 1024 129.8 us with eight, 123.4 with four)
+    // leave room for fewer wavefronts, which then hide less of the mask's arithmetic: 131072 bf16 rows of 1024 129.8 us with eight, 121.6 with four)
     constexpr int RB = sizeof(RowT) == 4 || EPI == EPI_DROP ? 4 : 8;
     typedef typename RowLoad<RowT, 1>::Raw Raw;
     const int d = p.d;

@@ -212,6 +212,8 @@ __device__ __forceinline__ uint32_t finite_size(float x)
 // looked at again without them.  Bound by memory, and so by how many tiles a compute unit holds: bf16 elements stay as they are, two to a register.
 // 8192 x 32768 bf16 to e5m2, both ways / rows only: 203 us = 5.3 TB/s / 142 = 5.7 (261 / 181 with fp32 in the registers and every magnitude by itself).
 // Two tiles, whose stretches are twice as long, against one: 205 / 210 us there, 8320 x 33152 219 / 234; against two below each other 205 / 212 and 219 / 226.
+// Rows of any length, whose 16-byte loads begin anywhere: 10001 x 10003 rows only / both ways 59 / 88 us of bf16, 116 / 141 of fp32, 5.3 and 4.8 TB/s by what is counted
+// rows only, of which lines that are read twice are 5 and 15 %.
 // Wavefronts to a SIMD: five of bf16, four of fp32, of which a fifth one makes more requests than memory takes well (8192 x 32768 rows only 273 us, so 281).
 template <typename T, int FMT, bool WHOLE, int WIDE>
 __global__ __launch_bounds__(256 * WIDE) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 5 : 4, sizeof(T) == 2 ? 5 : 4))) void quantize_kernel(Quantize p)
@@ -773,15 +775,18 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel([[maybe_unused]] 
                 for (int h = 0; h < MF; ++h) widen<FA>(v[h], sa[h] & 255u, wide[h]);
             }
         }
-        // The next tile's first blocks are on their way while this tile's result leaves through LDS, eight rows at a time, so that a wavefront stores whole
-        // stretches of 256 bytes; each has a place of its own, and waits for nobody.
+        // The next tile's first blocks are asked for before this tile's result leaves through LDS, eight rows at a time, so that a wavefront stores whole
+        // stretches of 256 bytes; each has a place of its own, and waits for nobody.  Results and loads overlap in the smaller tiles only.  256 x 256 tiles
+        // want more registers than there are (spilled: 8 to bf16, 2 to fp32, 28 onto a tensor), and what is read back behind the loads waits for them:
+        // nothing leaves before the blocks have arrived.
         wait_and_meet();
         const int64_t m_out = m0 + wm * MF * 16 + lane / VECS, n_out = n0 + wn * NF * 16 + (lane % VECS) * PER_VEC;
         const bool whole_tile = m_here == TM && n_here == TN, whole = whole_tile && !ONTO;
         const int64_t done = tile;
         const bool in_parts = done >= p.full && p.parts > 1;
         // c_in of a whole tile is asked for sixteen rows at a time (asked for where it is added, every store waited for it: 33801 x 1024 x 4987 onto fp32
-        // 331 us, so 305), by way of a buffer, whose addresses are one register for all rows.
+        // 331 us, so 305), by way of a buffer, whose addresses are one register for all rows.  (The stores' offsets are one for each row; in 256 x 256 tiles
+        // they are among what is spilled, and most stores wait behind a reload for the store before them.)
         const bool ahead = ONTO && whole_tile && p.N <= 1 << 20;
         const int64_t corner = (m0 + wm * MF * 16) * p.N + n0 + wn * NF * 16;
         const uint32_t row_bytes = (uint32_t)p.N * 4, from_corner = (uint32_t)(lane / VECS) * row_bytes + (uint32_t)(lane % VECS) * 16;
@@ -895,7 +900,7 @@ __global__ __launch_bounds__(64 * WN * WM) void parts_kernel(Matmul p)
     store4<HALF>(p, m, n, v);
 }
 
-// K = 0: out = c_in, or zeros; four bytes at a time.
+// K = 0: out = c_in, or zeros; an element to a lane.
 __global__ __launch_bounds__(256) void copy_kernel(const float* c_in, void* out, int64_t n, int elem, int64_t first_wg)
 {
     const int64_t at = (first_wg + blockIdx.x) * 256 + threadIdx.x;
@@ -984,7 +989,8 @@ Way way_for(int64_t M, int64_t N, int64_t K, bool half)
     const int blocks = (int)(code_row(K) / kBlock);
     Way w{FORM_ROWS, 1, blocks, 0, 0, 0, false};
     // Up to 32 rows the matrix instructions are idle anyway: B is read past LDS.  One wavefront has work for its latencies with eight blocks; where there are
-    // few places, up to four share one.  32 x 7003 x 512 to bf16 4.4 us, in tiles 5.6; 33 x 32768 x 1024 in tiles 10.4, in three fragments 13.
+    // few places, up to four share one.  32 rows / 33 rows, in tiles, us to bf16 and to fp32: 7003 x 512 5.3 / 6.0 and 5.6 / 7.2, 32768 x 1024 10.7 / 6.9 and
+    // 10.0 / 11.4, 1024 x 32768 55 / 16 and 49 / 18.  The limit is no part of the costs below; it loses where K is long, and at 32768 x 1024 to bf16.
     if (M <= 32) {
         const int64_t places = (N + 15) / 16;
         while (w.log_kw < 2 && (places << w.log_kw) < 2048 && (4 << w.log_kw) < blocks) ++w.log_kw;
